@@ -14,8 +14,8 @@ Where ``own`` is false, ``run`` computes the operators in elementary torch opera
 case alone, tensor values of the seed.
 
 The 4-bit cache: 32 consecutive channels of a row and head share a scale 2^e, held as the byte e + 127, where e is the least
-whole number with max|x| <= 7 * 2^e, no less than -125; a channel is a sign and one of the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4,
-6 (their index in 3 bits) of x / 2^e, the nearest, ties to the even index; channel 2i sits in the lower half of byte i.
+whole number with max|x| <= 7 * 2^e, between -125 and 125; a channel is a sign and one of the magnitudes 0, 0.5, 1, 1.5, 2, 3,
+4, 6 (their index in 3 bits) of x / 2^e, the nearest, ties to the even index; channel 2i sits in the lower half of byte i.
 A block with a NaN or an infinity has the scale byte 255 and reads as NaN.
 """
 from __future__ import annotations
@@ -180,7 +180,7 @@ def _quantise(x):
     bad = ~torch.isfinite(blocks).all(-1)
     mant, exp = torch.frexp(torch.where(bad, torch.ones_like(top), top))  # top = mant * 2^exp, mant in [0.5, 1)
     e = torch.where(mant <= 0.875, exp - 3, exp - 2)
-    e = torch.where(top == 0, torch.full_like(e, -125), e).clamp(-125, 127)
+    e = torch.where(top == 0, torch.full_like(e, -125), e).clamp(-125, 125)
     a = torch.ldexp(blocks.abs().double(), -e.unsqueeze(-1)).float()
     code = ((a > 0.25).int() + (a >= 0.75).int() + (a > 1.25).int() + (a >= 1.75).int() + (a > 2.5).int() + (a >= 3.5).int() +
             (a > 5.0).int())
@@ -424,7 +424,7 @@ def _nearest64(x):
     b = x.reshape(*x.shape[:-1], -1, 32)
     top = b.abs().max(dim=-1, keepdim=True).values
     e = torch.full_like(top, -125.0)
-    for step in range(-124, 128):  # the least e with top <= 7 * 2^e
+    for step in range(-124, 126):  # the least e with top <= 7 * 2^e
         e = torch.where(top > 7 * 2.0 ** (step - 1), torch.full_like(e, float(step)), e)
     a = b.abs() / torch.pow(2.0, e)
     grid = (0.0, 1.0, 2.0, 4.0, 0.5, 1.5, 3.0, 6.0)  # even indices first: they win ties
