@@ -370,6 +370,121 @@ int dodo_ste_score_grad(const void* Q, const void* Kn, const void* Vn, const voi
                         size_t ws_bytes, void* stream);
 
 /*
+ * Gradients of nugget attention (Eq. 13 / Eq. 9) in its inputs, from dO, the gradient of the loss in O, and from O and lse
+ * exactly as dodo_nugget_attention returned them for these inputs (lse is required there):
+ *   P[j,i] = exp(softmax_scale * q_j.k_i - lse[j]) where row j sees key i, else 0;   D[j] = dO[j].O[j],
+ *   dS[j,i] = P[j,i] * (dO[j].v_i - D[j]),
+ *   dQ[j] = softmax_scale * sum_i dS[j,i] k_i,   dK[i] = softmax_scale * sum_j dS[j,i] q_j,   dV[i] = sum_j P[j,i] dO[j],
+ * the sums of a K/V row running over all query heads that read it.  Q, dO, O, dQ are [Sq, H, d_h], lse fp32 [Sq, H];
+ * Kn, Vn, dKn, dVn the nugget cache in `layout` (Kt = cu_nuggets[B] rows); Kl, Vl, dKl, dVl [Sm, H_kv, d_h]; all but lse of
+ * `dtype`.  Sq, Kt, Sm are the total rows (host values); max_q / max_k / max_local bound q_b / k_b / m_b.  Every row of a
+ * sequence is written (0 where no query row sees it, or a query row that sees nothing); rows behind the last sequence are left
+ * as they are.  Inputs should be finite: a NaN or an infinity in a row reaches the gradients of its own sequence
+ * and no other's.
+ * Sums are fp32, the results rounded once; bf16 inputs are multiplied on the matrix cores with P and dS rounded to
+ * bf16, fp32 inputs in fp32.  Deterministic (fixed summation order, no atomics).  Supported: d_h in {64, 128}, fp32 or bf16.
+ * ws: dodo_nugget_attention_grad_workspace_bytes bytes, 16-byte aligned, contents irrelevant; a buffer of this size serves
+ * calls whose bounds and totals are all smaller too, and must not be shared by calls that may overlap in time.
+ */
+size_t dodo_nugget_attention_grad_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int32_t max_k,
+                                                  int32_t max_local, int64_t Sq, int64_t Kt, int64_t Sm, int dtype);
+int dodo_nugget_attention_grad(const void* Q, const void* Kn, const void* Vn, const void* Kl, const void* Vl, const void* dO,
+                               const void* O, const float* lse, const int32_t* cu_q, const int32_t* cu_nuggets,
+                               const int32_t* cu_local, int32_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q,
+                               int32_t max_k, int32_t max_local, int64_t Sq, int64_t Kt, int64_t Sm, float softmax_scale,
+                               int dtype, int layout, void* dQ, void* dKn, void* dVn, void* dKl, void* dVl, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/*
+ * The same for dodo_nugget_attention_segments: entry e has query rows seg_cu_q[e] .. seg_cu_q[e+1], nuggets
+ * seg_nug_start[e] .. + seg_nug_len[e] of the cache (Kt rows) and local rows seg_loc_start[e] .. + seg_loc_len[e] of K / V
+ * [N, H_kv, d_h].  Ranges of nuggets or of local rows may overlap: a row's gradient is the sum over the entries that hold it, in
+ * their order.  All Kt rows of dKn, dVn and all N rows of dK, dV are written, 0 where no entry holds the row; of dQ the rows
+ * from seg_cu_q[0] to seg_cu_q[n_segments].  (A text's total gradient of K and V has its nuggets' share too:
+ * dodo_gather_nuggets_grad with accumulate adds it.)  Here a NaN or an infinity may reach the gradients of other
+ * entries' K and V rows, up to 127 rows away from its own entry's.  The workspace is that of n_segments sequences with Sm = N.
+ */
+int dodo_nugget_attention_segments_grad(const void* Q, const void* Kn, const void* Vn, const void* K, const void* V,
+                                        const void* dO, const void* O, const float* lse, const int32_t* seg_cu_q,
+                                        const int32_t* seg_nug_start, const int32_t* seg_nug_len,
+                                        const int32_t* seg_loc_start, const int32_t* seg_loc_len, int32_t n_segments,
+                                        int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int32_t max_k,
+                                        int32_t max_local, int64_t Sq, int64_t Kt, int64_t N, float softmax_scale, int dtype,
+                                        int layout, void* dQ, void* dKn, void* dVn, void* dK, void* dV, void* ws,
+                                        size_t ws_bytes, void* stream);
+
+/*
+ * Gradient of dodo_gather_nuggets: the gradient rows of the nugget cache go back to the tokens that they were taken from.
+ * dKn, dVn are [Kt, H_kv, d_h] (token-major) or [H_kv, Kt, d_h] (head-major), dK, dV [N, H_kv, d_h] with
+ * `token_stride` elements between tokens.  accumulate = 0: every row of dK, dV that belongs to a sequence is written, with
+ * the sum of the nugget rows whose index it is, in list order (0 for a token that is no nugget); rows from cu_seqlens[B] on are
+ * left as they are.  accumulate != 0: these sums are added to the nuggets' tokens and no other row is touched.  nugget_idx holds the
+ * sequence-local indices in ascending order (dodo_select_topk, dodo_select_threshold), where an index may repeat; Kt =
+ * cu_nuggets[B] or an upper bound of it, with room for Kt entries in nugget_idx and Kt rows in dKn, dVn.  An index outside of its
+ * sequence is passed over.  Sums are fp32, rounded once; deterministic.
+ */
+int dodo_gather_nuggets_grad(const void* dKn, const void* dVn, int dtype, const int32_t* nugget_idx, const int32_t* cu_seqlens,
+                             const int32_t* cu_nuggets, int32_t B, int64_t Kt, int64_t N, int32_t H_kv, int32_t d_h,
+                             int64_t token_stride, int accumulate, void* dK, void* dV, int layout, void* stream);
+
+/* The same for the caches of L layers that share the index list (dodo_gather_nuggets_layers), in one launch: layer l reads
+ * dKn + l * src_layer_stride, dVn + l * src_layer_stride and writes dK + l * dst_layer_stride, dV + l * dst_layer_stride
+ * (elements, multiples of 16 bytes; src_layer_stride >= Kt * H_kv * d_h or 0, dst_layer_stride >= N * token_stride).  L <= 65535. */
+int dodo_gather_nuggets_grad_layers(const void* dKn, const void* dVn, int dtype, const int32_t* nugget_idx,
+                                    const int32_t* cu_seqlens, const int32_t* cu_nuggets, int32_t B, int64_t Kt, int64_t N,
+                                    int32_t L, int32_t H_kv, int32_t d_h, int64_t token_stride, int64_t src_layer_stride,
+                                    int64_t dst_layer_stride, int accumulate, void* dK, void* dV, int layout, void* stream);
+
+/*
+ * Nugget caches in 4 bits.  32 consecutive channels of a row and head (a block) share a scale 2^e, held as the byte e + 127; a
+ * channel x is a sign (bit 3) and the index (bits 0..2) of one of the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6: the nearest to
+ * |x| / 2^e, ties to the even index.  e is the least whole number with max|x| <= 7 * 2^e -- the largest value is then off by
+ * at most half of a step of 2 -- held between -125 and 125.  A block with a NaN or an infinity gets the scale byte 255, which makes
+ * all of its channels read as NaN (its codes are 0).  Channel 2i sits in the lower four bits of byte i.  A row and head take
+ * d_h / 2 + d_h / 32 bytes (4.25 bits a channel, 3.76 times less than bf16), codes and scales in two arrays:
+ *   Kc, Vc  [Kt, H_kv, d_h / 2] (token-major) or [H_kv, Kt, d_h / 2] (head-major) bytes, 16-byte aligned
+ *   Ks, Vs  [Kt, H_kv, d_h / 32] or [H_kv, Kt, d_h / 32] bytes, 4-byte aligned
+ * Every value is a bf16 number (and an fp32 one), so that reading a cache back rounds nothing.
+ *
+ * dodo_gather_nuggets_q4 is dodo_gather_nuggets into such a cache (d_h a multiple of 32).
+ */
+int dodo_gather_nuggets_q4(const void* K, const void* V, int dtype, const int32_t* nugget_idx, const int32_t* cu_seqlens,
+                           const int32_t* cu_nuggets, int32_t B, int64_t Kt, int32_t H_kv, int32_t d_h, int64_t token_stride,
+                           uint8_t* Kc, uint8_t* Ks, uint8_t* Vc, uint8_t* Vs, int layout, void* stream);
+
+/* The same for L layers that share the index list, in one launch: layer l reads K + l * src_layer_stride and V +
+ * l * src_layer_stride (elements, a multiple of 16 bytes) and writes the caches of layer l, which lie one after the other:
+ * Kc, Vc [L, Kt * H_kv * d_h / 2], Ks, Vs [L, Kt * H_kv * d_h / 32].  L <= 65535. */
+int dodo_gather_nuggets_q4_layers(const void* K, const void* V, int dtype, const int32_t* nugget_idx, const int32_t* cu_seqlens,
+                                  const int32_t* cu_nuggets, int32_t B, int64_t Kt, int32_t L, int32_t H_kv, int32_t d_h,
+                                  int64_t token_stride, int64_t src_layer_stride, uint8_t* Kc, uint8_t* Ks, uint8_t* Vc,
+                                  uint8_t* Vs, int layout, void* stream);
+
+/*
+ * What a 4-bit cache stands for, as a plain one of `dtype`: `rows` rows and heads (Kt * H_kv, of all layers together, in either
+ * layout) of d_h channels (a multiple of 32) each.  Kn, Vn have the order of Kc, Vc.  rows == 0 is a no-op.
+ */
+int dodo_unpack_nuggets_q4(const uint8_t* Kc, const uint8_t* Ks, const uint8_t* Vc, const uint8_t* Vs, int64_t rows, int32_t d_h,
+                           int dtype, void* Kn, void* Vn, void* stream);
+
+/*
+ * dodo_nugget_attention over a nugget cache in 4 bits (Kc, Ks, Vc, Vs in `layout`, Kt rows); the local rows, Q and O are of
+ * `dtype`.  Same arguments, causal rule and result as dodo_nugget_attention over the unpacked cache: logits, sums and
+ * the weights' products are fp32 sums of exact products of bf16 numbers, whose weights are rounded as there.  Supported:
+ * d_h in {64, 128}, fp32 or bf16.
+ * ws: dodo_nugget_attention_q4_workspace_bytes bytes, 16-byte aligned, zero-filled before its first use; a call leaves it so that
+ * calls with the same arguments can use it again as it is (fill it with zeros before a call with other ones, and after a
+ * call that was aborted).  It must not be shared by calls that may overlap in time.
+ */
+size_t dodo_nugget_attention_q4_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int32_t max_k,
+                                                int32_t max_local, int64_t Kt, int dtype);
+int dodo_nugget_attention_q4(const void* Q, const uint8_t* Kc, const uint8_t* Ks, const uint8_t* Vc, const uint8_t* Vs,
+                             const void* Kl, const void* Vl, const int32_t* cu_q, const int32_t* cu_nuggets,
+                             const int32_t* cu_local, int32_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q,
+                             int32_t max_k, int32_t max_local, int64_t Kt, float softmax_scale, int dtype, int layout, void* O,
+                             float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Threshold of the autoregressive mode from sampled scores (Sec. 2.4: Lambda is set so that about
  * t/r of t tokens are kept, and is estimated by running the scorer on sampled tokens).  With
  * k = dodo_nugget_count(n, num, den), writes to *lambda_out (device, fp32) the (k+1)-th highest

@@ -93,6 +93,30 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.dodo_nugget_attention_cached.restype = ctypes.c_int
     L.dodo_nugget_attention_cached.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
                                                i64, f32, ctypes.c_int, ctypes.c_int, vp, vp, vp, sz, vp]
+    L.dodo_nugget_attention_grad_workspace_bytes.restype = sz
+    L.dodo_nugget_attention_grad_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32, i64, i64, i64, ctypes.c_int]
+    L.dodo_nugget_attention_grad.restype = ctypes.c_int
+    L.dodo_nugget_attention_grad.argtypes = [vp] * 11 + [i32] * 7 + [i64] * 3 + [f32, ctypes.c_int, ctypes.c_int] + [vp] * 6 + [sz, vp]
+    L.dodo_nugget_attention_segments_grad.restype = ctypes.c_int
+    L.dodo_nugget_attention_segments_grad.argtypes = ([vp] * 13 + [i32] * 7 + [i64] * 3 + [f32, ctypes.c_int, ctypes.c_int] + [vp] * 6 +
+                                                      [sz, vp])
+    L.dodo_gather_nuggets_grad.restype = ctypes.c_int
+    L.dodo_gather_nuggets_grad.argtypes = [vp, vp, ctypes.c_int, vp, vp, vp, i32, i64, i64, i32, i32, i64, ctypes.c_int, vp, vp,
+                                           ctypes.c_int, vp]
+    L.dodo_gather_nuggets_grad_layers.restype = ctypes.c_int
+    L.dodo_gather_nuggets_grad_layers.argtypes = [vp, vp, ctypes.c_int, vp, vp, vp, i32, i64, i64, i32, i32, i32, i64, i64, i64,
+                                                  ctypes.c_int, vp, vp, ctypes.c_int, vp]
+    L.dodo_gather_nuggets_q4.restype = ctypes.c_int
+    L.dodo_gather_nuggets_q4.argtypes = [vp, vp, ctypes.c_int, vp, vp, vp, i32, i64, i32, i32, i64, vp, vp, vp, vp, ctypes.c_int, vp]
+    L.dodo_gather_nuggets_q4_layers.restype = ctypes.c_int
+    L.dodo_gather_nuggets_q4_layers.argtypes = [vp, vp, ctypes.c_int, vp, vp, vp, i32, i64, i32, i32, i32, i64, i64, vp, vp, vp, vp,
+                                                ctypes.c_int, vp]
+    L.dodo_unpack_nuggets_q4.restype = ctypes.c_int
+    L.dodo_unpack_nuggets_q4.argtypes = [vp, vp, vp, vp, i64, i32, ctypes.c_int, vp, vp, vp]
+    L.dodo_nugget_attention_q4_workspace_bytes.restype = sz
+    L.dodo_nugget_attention_q4_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32, i64, ctypes.c_int]
+    L.dodo_nugget_attention_q4.restype = ctypes.c_int
+    L.dodo_nugget_attention_q4.argtypes = [vp] * 10 + [i32] * 7 + [i64, f32, ctypes.c_int, ctypes.c_int, vp, vp, vp, sz, vp]
     L.dodo_threshold_from_sample.restype = ctypes.c_int
     L.dodo_threshold_from_sample.argtypes = [vp, i64, i64, i64, vp, vp, sz, vp]
     L.dodo_threshold_from_sample_workspace_bytes.restype = sz
@@ -171,6 +195,36 @@ def _dev_rows(*ts: torch.Tensor) -> None:
             inner *= size
         if not t.is_cuda or (t.shape[0] > 1 and t.stride(0) < inner):
             raise ValueError("dodo tensors must be device tensors with a row stride of at least a row")
+
+
+def _same_device(first: torch.Tensor, *ts: Optional[torch.Tensor]) -> None:
+    """All of them on the current device, whose current stream the call goes to."""
+    for t in (first, *ts):
+        if t is not None and (not t.is_cuda or t.device.index != _current_device()):
+            raise ValueError("dodo tensors must be on the current device")
+
+
+def _int32(*ts: torch.Tensor) -> None:
+    for t in ts:
+        if t.dtype != torch.int32 or t.dim() != 1:
+            raise TypeError("dodo takes starts, lengths and index lists as int32 arrays")
+
+
+def _shape(t: torch.Tensor, shape: tuple, dtype: torch.dtype, name: str) -> None:
+    if tuple(t.shape) != shape or t.dtype != dtype:
+        raise ValueError(f"{name} has to be {list(shape)} of {dtype}, got {list(t.shape)} of {t.dtype}")
+
+
+def _like(t: Optional[torch.Tensor], model: torch.Tensor, name: str) -> torch.Tensor:
+    """The caller's output, or a new one, in the shape and type of `model`."""
+    if t is None:
+        return torch.empty(model.shape, dtype=model.dtype, device=model.device)
+    _shape(t, tuple(model.shape), model.dtype, name)
+    return t
+
+
+def _workspace(ws: Optional[torch.Tensor]) -> Tuple[int, int]:
+    return _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size()
 
 
 def dodo_version() -> int:
@@ -542,6 +596,254 @@ def dodo_nugget_attention_cached(Q: torch.Tensor, Kn: torch.Tensor, Vn: torch.Te
                                             max_q, max_k, max_local, Kt, float(softmax_scale), code, layout, _ptr(O),
                                             _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream()),
            "dodo_nugget_attention_cached")
+    return O, lse
+
+
+def dodo_nugget_attention_grad_workspace_bytes(B: int, H: int, H_kv: int, d_h: int, max_q: int, max_k: int, max_local: int, Sq: int,
+                                               Kt: int, Sm: int, dtype: int) -> int:
+    return int(lib.dodo_nugget_attention_grad_workspace_bytes(B, H, H_kv, d_h, max_q, max_k, max_local, Sq, Kt, Sm, dtype))
+
+
+def _attention_grad(call, where: str, Q, Kn, Vn, Kl, Vl, dO, O, lse, ranges, B, max_q, max_k, max_local, softmax_scale, layout, dQ, dKn,
+                    dVn, dKl, dVl, ws):
+    _same_device(Q, Kn, Vn, Kl, Vl, dO, O, lse, *ranges, dQ, dKn, dVn, dKl, dVl, ws)
+    _dev(Q, Kn, Vn, Kl, Vl, dO, O, lse, *ranges, dQ, dKn, dVn, dKl, dVl, ws)
+    _int32(*ranges)
+    Sq, H, d_h = Q.shape
+    Sm, H_kv, _ = Kl.shape
+    Kt = Kn.shape[0] if layout == TOKEN_MAJOR else Kn.shape[1]
+    cache = (Kt, H_kv, d_h) if layout == TOKEN_MAJOR else (H_kv, Kt, d_h)
+    for name, t, shape, dtype in (("dO", dO, (Sq, H, d_h), Q.dtype), ("O", O, (Sq, H, d_h), Q.dtype), ("lse", lse, (Sq, H), torch.float32),
+                                  ("Kn", Kn, cache, Q.dtype), ("Vn", Vn, cache, Q.dtype), ("Kl", Kl, (Sm, H_kv, d_h), Q.dtype),
+                                  ("Vl", Vl, (Sm, H_kv, d_h), Q.dtype)):
+        _shape(t, shape, dtype, name)
+    if softmax_scale is None:
+        softmax_scale = 1.0 / math.sqrt(d_h)
+    dQ, dKn, dVn, dKl, dVl = _like(dQ, Q, "dQ"), _like(dKn, Kn, "dKn"), _like(dVn, Vn, "dVn"), _like(dKl, Kl, "dKl"), _like(dVl, Vl, "dVl")
+    code = _dtype_code(Q)
+    need = dodo_nugget_attention_grad_workspace_bytes(B, H, H_kv, d_h, max_q, max_k, max_local, Sq, Kt, Sm, code)
+    if need and ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
+    _check(call(_ptr(Q), _ptr(Kn), _ptr(Vn), _ptr(Kl), _ptr(Vl), _ptr(dO), _ptr(O), _ptr(lse), *(_ptr(r) for r in ranges), B, H, H_kv, d_h,
+                max_q, max_k, max_local, Sq, Kt, Sm, float(softmax_scale), code, layout, _ptr(dQ), _ptr(dKn), _ptr(dVn), _ptr(dKl),
+                _ptr(dVl), *_workspace(ws), _stream()), where)
+    return dQ, dKn, dVn, dKl, dVl
+
+
+def dodo_nugget_attention_grad(Q: torch.Tensor, Kn: torch.Tensor, Vn: torch.Tensor, Kl: torch.Tensor, Vl: torch.Tensor, dO: torch.Tensor,
+                               O: torch.Tensor, lse: torch.Tensor, cu_q: torch.Tensor, cu_nuggets: torch.Tensor, cu_local: torch.Tensor,
+                               max_q: int, max_k: int, max_local: int, softmax_scale: Optional[float] = None, layout: int = TOKEN_MAJOR,
+                               dQ: Optional[torch.Tensor] = None, dKn: Optional[torch.Tensor] = None, dVn: Optional[torch.Tensor] = None,
+                               dKl: Optional[torch.Tensor] = None, dVl: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """Gradients of dodo_nugget_attention from dO, with its O and lse; returns (dQ, dKn, dVn, dKl, dVl) in the inputs' shapes."""
+    if not cu_q.numel() == cu_nuggets.numel() == cu_local.numel():
+        raise ValueError("cu_q, cu_nuggets and cu_local have to be of one length")
+    return _attention_grad(lib.dodo_nugget_attention_grad, "dodo_nugget_attention_grad", Q, Kn, Vn, Kl, Vl, dO, O, lse,
+                           (cu_q, cu_nuggets, cu_local), cu_q.numel() - 1, max_q, max_k, max_local, softmax_scale, layout, dQ, dKn, dVn,
+                           dKl, dVl, ws)
+
+
+def dodo_nugget_attention_segments_grad(Q: torch.Tensor, Kn: torch.Tensor, Vn: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
+                                        dO: torch.Tensor, O: torch.Tensor, lse: torch.Tensor, seg_cu_q: torch.Tensor,
+                                        seg_nug_start: torch.Tensor, seg_nug_len: torch.Tensor, seg_loc_start: torch.Tensor,
+                                        seg_loc_len: torch.Tensor, max_q: int, max_k: int, max_local: int,
+                                        softmax_scale: Optional[float] = None, layout: int = TOKEN_MAJOR,
+                                        dQ: Optional[torch.Tensor] = None, dKn: Optional[torch.Tensor] = None,
+                                        dVn: Optional[torch.Tensor] = None, dK: Optional[torch.Tensor] = None,
+                                        dV: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """Gradients of dodo_nugget_attention_segments, those of shared rows summed over the entries; returns (dQ, dKn, dVn, dK, dV)."""
+    n_seg = seg_cu_q.numel() - 1
+    for t in (seg_nug_start, seg_nug_len, seg_loc_start, seg_loc_len):
+        if t.numel() != n_seg:
+            raise ValueError("seg_cu_q has to have one entry more than the segments' starts and lengths")
+    return _attention_grad(lib.dodo_nugget_attention_segments_grad, "dodo_nugget_attention_segments_grad", Q, Kn, Vn, K, V, dO, O, lse,
+                           (seg_cu_q, seg_nug_start, seg_nug_len, seg_loc_start, seg_loc_len), n_seg, max_q, max_k, max_local,
+                           softmax_scale, layout, dQ, dKn, dVn, dK, dV, ws)
+
+
+def dodo_gather_nuggets_grad(dKn: torch.Tensor, dVn: torch.Tensor, nugget_idx: torch.Tensor, cu_seqlens: torch.Tensor,
+                             cu_nuggets: torch.Tensor, total_tokens: int, layout: int = TOKEN_MAJOR, dK: Optional[torch.Tensor] = None,
+                             dV: Optional[torch.Tensor] = None, accumulate: bool = False):
+    """Gradient of dodo_gather_nuggets: the cache's gradient rows back at their tokens, zeros elsewhere; with accumulate they are
+    added to dK, dV instead.  Returns (dK, dV) [N, H_kv, d_h]."""
+    _same_device(dKn, dVn, nugget_idx, cu_seqlens, cu_nuggets, dK, dV)
+    _dev(dKn, dVn, nugget_idx, cu_seqlens, cu_nuggets)
+    _int32(nugget_idx, cu_seqlens, cu_nuggets)
+    Kt, H_kv, d_h = dKn.shape if layout == TOKEN_MAJOR else (dKn.shape[1], dKn.shape[0], dKn.shape[2])
+    _shape(dVn, tuple(dKn.shape), dKn.dtype, "dVn")
+    if (dK is None or dV is None) and (accumulate or dK is not dV):
+        raise ValueError("give both of dK and dV, or neither (accumulate adds to them)")
+    if nugget_idx.numel() < Kt or cu_nuggets.numel() != cu_seqlens.numel():
+        raise ValueError("nugget_idx has to hold an index per cache row, cu_nuggets an entry per sequence")
+    if dK is None:
+        dK, dV = (torch.empty((total_tokens, H_kv, d_h), dtype=dKn.dtype, device=dKn.device) for _ in range(2))
+    _dev_rows(dK, dV)
+    for name, t in (("dK", dK), ("dV", dV)):
+        _shape(t, (total_tokens, H_kv, d_h), dKn.dtype, name)
+    if dK.stride() != dV.stride():
+        raise ValueError("dK and dV have to have the same strides")
+    _check(lib.dodo_gather_nuggets_grad(_ptr(dKn), _ptr(dVn), _dtype_code(dKn), _ptr(nugget_idx), _ptr(cu_seqlens), _ptr(cu_nuggets),
+                                        cu_seqlens.numel() - 1, Kt, total_tokens, H_kv, d_h, _row_stride(dK), int(bool(accumulate)),
+                                        _ptr(dK), _ptr(dV), layout, _stream()), "dodo_gather_nuggets_grad")
+    return dK, dV
+
+
+def _row_stride(t: torch.Tensor, dim: int = 0) -> int:
+    """Elements between the rows of t along `dim`, at least a row (a single row's stride means nothing)."""
+    return t.stride(dim) if t.shape[dim] > 1 else math.prod(t.shape[dim + 1:])
+
+
+def _layered(name: str, *ts: torch.Tensor) -> None:
+    """Tensors [L, rows, H, d] with contiguous rows of one stride, layers apart by one stride."""
+    for t in ts:
+        if t.dim() != 4 or t.stride() != ts[0].stride():
+            raise ValueError(f"{name} have to be [L, rows, H_kv, d_h] with the same strides")
+        if t.shape[0] > 0:
+            _dev_rows(t[0])
+
+
+def dodo_gather_nuggets_grad_layers(dKn: torch.Tensor, dVn: torch.Tensor, nugget_idx: torch.Tensor, cu_seqlens: torch.Tensor,
+                                    cu_nuggets: torch.Tensor, total_tokens: int, layout: int = TOKEN_MAJOR,
+                                    dK: Optional[torch.Tensor] = None, dV: Optional[torch.Tensor] = None, accumulate: bool = False):
+    """dodo_gather_nuggets_grad for the caches of L layers [L, ...] in one launch; returns (dK, dV) [L, N, H_kv, d_h]."""
+    _same_device(dKn, dVn, nugget_idx, cu_seqlens, cu_nuggets, dK, dV)
+    _dev(dKn, dVn, nugget_idx, cu_seqlens, cu_nuggets)
+    _int32(nugget_idx, cu_seqlens, cu_nuggets)
+    L = dKn.shape[0]
+    Kt, H_kv, d_h = dKn.shape[1:] if layout == TOKEN_MAJOR else (dKn.shape[2], dKn.shape[1], dKn.shape[3])
+    _shape(dVn, tuple(dKn.shape), dKn.dtype, "dVn")
+    if (dK is None or dV is None) and (accumulate or dK is not dV):
+        raise ValueError("give both of dK and dV, or neither (accumulate adds to them)")
+    if nugget_idx.numel() < Kt or cu_nuggets.numel() != cu_seqlens.numel():
+        raise ValueError("nugget_idx has to hold an index per cache row, cu_nuggets an entry per sequence")
+    if dK is None:
+        dK, dV = (torch.empty((L, total_tokens, H_kv, d_h), dtype=dKn.dtype, device=dKn.device) for _ in range(2))
+    for name, t in (("dK", dK), ("dV", dV)):
+        _shape(t, (L, total_tokens, H_kv, d_h), dKn.dtype, name)
+    _layered("dK and dV", dK, dV)
+    row = _row_stride(dK, 1)
+    _check(lib.dodo_gather_nuggets_grad_layers(_ptr(dKn), _ptr(dVn), _dtype_code(dKn), _ptr(nugget_idx), _ptr(cu_seqlens),
+                                               _ptr(cu_nuggets), cu_seqlens.numel() - 1, Kt, total_tokens, L, H_kv, d_h, row,
+                                               Kt * H_kv * d_h, dK.stride(0), int(bool(accumulate)), _ptr(dK), _ptr(dV), layout,
+                                               _stream()), "dodo_gather_nuggets_grad_layers")
+    return dK, dV
+
+
+def _q4_cache(lead: tuple, H_kv: int, Kt: int, d_h: int, layout: int, outs, device):
+    """The caller's codes and scales of K and V, or new ones, in the shapes of a 4-bit cache."""
+    rows = (Kt, H_kv) if layout == TOKEN_MAJOR else (H_kv, Kt)
+    shapes = [lead + rows + (d_h // 2,), lead + rows + (d_h // 32,)] * 2
+    if all(o is None for o in outs):
+        return [torch.empty(s, dtype=torch.uint8, device=device) for s in shapes]
+    for name, o, s in zip(("Kc", "Ks", "Vc", "Vs"), outs, shapes):
+        if o is None:
+            raise ValueError("give all of Kc, Ks, Vc, Vs or none")
+        _shape(o, s, torch.uint8, name)
+    return list(outs)
+
+
+def dodo_gather_nuggets_q4(K: torch.Tensor, V: torch.Tensor, nugget_idx: torch.Tensor, cu_seqlens: torch.Tensor, cu_nuggets: torch.Tensor,
+                           total_nuggets: int, layout: int = TOKEN_MAJOR, Kc: Optional[torch.Tensor] = None,
+                           Ks: Optional[torch.Tensor] = None, Vc: Optional[torch.Tensor] = None, Vs: Optional[torch.Tensor] = None):
+    """Packs the chosen rows of K, V [N, H_kv, d_h] into a nugget cache in 4 bits; returns codes and scales (Kc, Ks, Vc, Vs)."""
+    _same_device(K, V, nugget_idx, cu_seqlens, cu_nuggets, Kc, Ks, Vc, Vs)
+    _dev(nugget_idx, cu_seqlens, cu_nuggets, Kc, Ks, Vc, Vs)
+    _dev_rows(K, V)
+    _int32(nugget_idx, cu_seqlens, cu_nuggets)
+    N, H_kv, d_h = K.shape
+    _shape(V, tuple(K.shape), K.dtype, "V")
+    if V.stride() != K.stride():
+        raise ValueError("K and V have to have the same strides")
+    if nugget_idx.numel() < total_nuggets or cu_nuggets.numel() != cu_seqlens.numel():
+        raise ValueError("nugget_idx has to hold an index per cache row, cu_nuggets an entry per sequence")
+    out = _q4_cache((), H_kv, total_nuggets, d_h, layout, (Kc, Ks, Vc, Vs), K.device)
+    _check(lib.dodo_gather_nuggets_q4(_ptr(K), _ptr(V), _dtype_code(K), _ptr(nugget_idx), _ptr(cu_seqlens), _ptr(cu_nuggets),
+                                      cu_seqlens.numel() - 1, total_nuggets, H_kv, d_h, _row_stride(K), *(_ptr(o) for o in out), layout,
+                                      _stream()), "dodo_gather_nuggets_q4")
+    return tuple(out)
+
+
+def dodo_gather_nuggets_q4_layers(K: torch.Tensor, V: torch.Tensor, nugget_idx: torch.Tensor, cu_seqlens: torch.Tensor,
+                                  cu_nuggets: torch.Tensor, total_nuggets: int, layout: int = TOKEN_MAJOR,
+                                  Kc: Optional[torch.Tensor] = None, Ks: Optional[torch.Tensor] = None, Vc: Optional[torch.Tensor] = None,
+                                  Vs: Optional[torch.Tensor] = None):
+    """dodo_gather_nuggets_q4 for the K, V [L, N, H_kv, d_h] of L layers (one shared index list) in one launch."""
+    _same_device(K, V, nugget_idx, cu_seqlens, cu_nuggets, Kc, Ks, Vc, Vs)
+    _dev(nugget_idx, cu_seqlens, cu_nuggets, Kc, Ks, Vc, Vs)
+    _int32(nugget_idx, cu_seqlens, cu_nuggets)
+    L, N, H_kv, d_h = K.shape
+    _shape(V, tuple(K.shape), K.dtype, "V")
+    _layered("K and V", K, V)
+    if nugget_idx.numel() < total_nuggets or cu_nuggets.numel() != cu_seqlens.numel():
+        raise ValueError("nugget_idx has to hold an index per cache row, cu_nuggets an entry per sequence")
+    out = _q4_cache((L,), H_kv, total_nuggets, d_h, layout, (Kc, Ks, Vc, Vs), K.device)
+    _check(lib.dodo_gather_nuggets_q4_layers(_ptr(K), _ptr(V), _dtype_code(K), _ptr(nugget_idx), _ptr(cu_seqlens), _ptr(cu_nuggets),
+                                             cu_seqlens.numel() - 1, total_nuggets, L, H_kv, d_h, _row_stride(K, 1), K.stride(0),
+                                             *(_ptr(o) for o in out), layout, _stream()), "dodo_gather_nuggets_q4_layers")
+    return tuple(out)
+
+
+def dodo_unpack_nuggets_q4(Kc: torch.Tensor, Ks: torch.Tensor, Vc: torch.Tensor, Vs: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
+                           Kn: Optional[torch.Tensor] = None, Vn: Optional[torch.Tensor] = None):
+    """The plain nugget cache (of `dtype`) that a 4-bit one stands for, in its layout (any leading dimensions); returns (Kn, Vn)."""
+    _same_device(Kc, Ks, Vc, Vs, Kn, Vn)
+    _dev(Kc, Ks, Vc, Vs, Kn, Vn)
+    d_h = 2 * Kc.shape[-1]
+    _shape(Vc, tuple(Kc.shape), torch.uint8, "Vc")
+    for name, t in (("Ks", Ks), ("Vs", Vs)):
+        _shape(t, tuple(Kc.shape[:-1]) + (d_h // 32,), torch.uint8, name)
+    _shape(Kc, tuple(Kc.shape), torch.uint8, "Kc")
+    shape = tuple(Kc.shape[:-1]) + (d_h,)
+    if Kn is None:
+        Kn = torch.empty(shape, dtype=dtype, device=Kc.device)
+    if Vn is None:
+        Vn = torch.empty(shape, dtype=dtype, device=Kc.device)
+    _shape(Kn, shape, dtype, "Kn")
+    _shape(Vn, shape, dtype, "Vn")
+    _check(lib.dodo_unpack_nuggets_q4(_ptr(Kc), _ptr(Ks), _ptr(Vc), _ptr(Vs), math.prod(Kc.shape[:-1]), d_h, _dtype_code(Kn), _ptr(Kn),
+                                      _ptr(Vn), _stream()), "dodo_unpack_nuggets_q4")
+    return Kn, Vn
+
+
+def dodo_nugget_attention_q4_workspace_bytes(B: int, H: int, H_kv: int, d_h: int, max_q: int, max_k: int, max_local: int, Kt: int,
+                                             dtype: int) -> int:
+    return int(lib.dodo_nugget_attention_q4_workspace_bytes(B, H, H_kv, d_h, max_q, max_k, max_local, Kt, dtype))
+
+
+def dodo_nugget_attention_q4(Q: torch.Tensor, Kc: torch.Tensor, Ks: torch.Tensor, Vc: torch.Tensor, Vs: torch.Tensor, Kl: torch.Tensor,
+                             Vl: torch.Tensor, cu_q: torch.Tensor, cu_nuggets: torch.Tensor, cu_local: torch.Tensor, max_q: int,
+                             max_k: int, max_local: int, softmax_scale: Optional[float] = None, layout: int = TOKEN_MAJOR,
+                             O: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                             ws: Optional[torch.Tensor] = None):
+    """dodo_nugget_attention over a nugget cache in 4 bits (codes and scales of K and V); returns (O, lse or None)."""
+    _same_device(Q, Kc, Ks, Vc, Vs, Kl, Vl, cu_q, cu_nuggets, cu_local, O, lse, ws)
+    _dev(Q, Kc, Ks, Vc, Vs, Kl, Vl, cu_q, cu_nuggets, cu_local, O, lse, ws)
+    _int32(cu_q, cu_nuggets, cu_local)
+    Sq, H, d_h = Q.shape
+    Sm, H_kv, _ = Kl.shape
+    Kt = Kc.shape[0] if layout == TOKEN_MAJOR else Kc.shape[1]
+    rows = (Kt, H_kv) if layout == TOKEN_MAJOR else (H_kv, Kt)
+    for name, t, shape, dtype in (("Kc", Kc, rows + (d_h // 2,), torch.uint8), ("Vc", Vc, rows + (d_h // 2,), torch.uint8),
+                                  ("Ks", Ks, rows + (d_h // 32,), torch.uint8), ("Vs", Vs, rows + (d_h // 32,), torch.uint8),
+                                  ("Kl", Kl, (Sm, H_kv, d_h), Q.dtype), ("Vl", Vl, (Sm, H_kv, d_h), Q.dtype)):
+        _shape(t, shape, dtype, name)
+    if not cu_q.numel() == cu_nuggets.numel() == cu_local.numel():
+        raise ValueError("cu_q, cu_nuggets and cu_local have to be of one length")
+    B = cu_q.numel() - 1
+    if softmax_scale is None:
+        softmax_scale = 1.0 / math.sqrt(d_h)
+    O = _like(O, Q, "O")
+    if lse is None and want_lse:
+        lse = torch.empty((Sq, H), dtype=torch.float32, device=Q.device)
+    if lse is not None:
+        _shape(lse, (Sq, H), torch.float32, "lse")
+    code = _dtype_code(Q)
+    need = dodo_nugget_attention_q4_workspace_bytes(B, H, H_kv, d_h, max_q, max_k, max_local, Kt, code)
+    if need and ws is None:
+        ws = torch.zeros(need, dtype=torch.uint8, device=Q.device)
+    _check(lib.dodo_nugget_attention_q4(_ptr(Q), _ptr(Kc), _ptr(Ks), _ptr(Vc), _ptr(Vs), _ptr(Kl), _ptr(Vl), _ptr(cu_q), _ptr(cu_nuggets),
+                                        _ptr(cu_local), B, H, H_kv, d_h, max_q, max_k, max_local, Kt, float(softmax_scale), code, layout,
+                                        _ptr(O), _ptr(lse), *_workspace(ws), _stream()), "dodo_nugget_attention_q4")
     return O, lse
 
 

@@ -1,0 +1,119 @@
+// What the kernels of dodo_nugget_attention_grad share: arguments, the ranges of an entry, tiles of keys.
+#pragma once
+#include "dodo_common.h"
+
+namespace dodo {
+
+constexpr int kGradWaves = 4;
+constexpr int kGradThreads = kGradWaves * kWave;
+
+struct GradParams {
+  const void *Q, *Kn, *Vn, *Kl, *Vl, *dO;
+  const float *lse2, *D;  // [H][Sq]
+  const int32_t *cu_q, *cu_nuggets, *cu_local;
+  const int32_t *nug_len, *loc_len;  // null: ranges end where the next begins
+  int shared;                        // != 0: entries may share rows, so that key tiles run over all rows instead of a sequence's
+  int32_t B, H, H_kv, max_q, max_k, max_local;
+  int64_t Sq, Kt, Sm;
+  int64_t nug_tok_stride, nug_head_stride, loc_tok_stride, loc_head_stride;  // elements
+  float scale, scale_log2e;
+  void *dQ, *dKn, *dVn, *dKl, *dVl;
+  hipStream_t stream;
+};
+
+// Rows of entry e: queries, nuggets, local rows.
+struct Entry {
+  int q0, q_b, k0, k_b, l0, m_b;
+};
+__device__ __forceinline__ Entry entry_of(const GradParams& p, int e) {
+  Entry s;
+  s.q0 = p.cu_q[e];
+  s.q_b = p.cu_q[e + 1] - s.q0;
+  s.k0 = p.cu_nuggets[e];
+  s.k_b = p.nug_len != nullptr ? p.nug_len[e] : p.cu_nuggets[e + 1] - s.k0;
+  s.l0 = p.cu_local[e];
+  s.m_b = p.loc_len != nullptr ? p.loc_len[e] : p.cu_local[e + 1] - s.l0;
+  return s;
+}
+
+// `rows` consecutive key rows of a K/V head from `first` on, in the nugget cache or among the local rows, and the entries
+// that may see them.
+struct KeyTile {
+  const void *K, *V;
+  void *dK, *dV;
+  int64_t first, tok_stride, head_stride;
+  int rows, kvh, entry0, entry1;
+  bool local;
+};
+// Tile `item` of a grid of (n_nug_tiles + n_loc_tiles) tiles of `size` rows per K/V head (and sequence, unless rows are shared);
+// rows <= 0: nothing there.
+__device__ __forceinline__ KeyTile key_tile(const GradParams& p, unsigned item, int n_nug_tiles, int n_loc_tiles, int size) {
+  KeyTile t;
+  const unsigned tiles = n_nug_tiles + n_loc_tiles;
+  int tile = item % tiles;
+  const unsigned rest = item / tiles;
+  t.kvh = rest % p.H_kv;
+  const int b = rest / p.H_kv;
+  t.local = tile >= n_nug_tiles;
+  if (t.local) tile -= n_nug_tiles;
+  int64_t begin = 0, end = t.local ? p.Sm : p.Kt;
+  if (!p.shared) {
+    const Entry s = entry_of(p, b);
+    begin = t.local ? s.l0 : s.k0;
+    end = begin + (t.local ? s.m_b : s.k_b);
+  }
+  t.first = begin + static_cast<int64_t>(tile) * size;
+  t.rows = static_cast<int>(min(static_cast<int64_t>(size), end - t.first));
+  t.entry0 = p.shared ? 0 : b;
+  t.entry1 = p.shared ? p.B : b + 1;
+  t.K = t.local ? p.Kl : p.Kn;
+  t.V = t.local ? p.Vl : p.Vn;
+  t.dK = t.local ? p.dKl : p.dKn;
+  t.dV = t.local ? p.dVl : p.dVn;
+  t.tok_stride = t.local ? p.loc_tok_stride : p.nug_tok_stride;
+  t.head_stride = t.local ? p.loc_head_stride : p.nug_head_stride;
+  return t;
+}
+
+// Which query rows of an entry see a tile's keys: key j of the entry (of len from row key0 on) is seen by the query rows from
+// max(0, j - lag) on, up to q_b.
+struct SeenBy {
+  int q0, q_b, len, lag, first_row;
+  int64_t key0;
+  bool any;
+  __device__ __forceinline__ int least(int j, bool ok) const { return ok && j >= 0 && j < len ? max(0, j - lag) : 0x7fffffff; }
+};
+__device__ __forceinline__ SeenBy seen_by(const GradParams& p, const KeyTile& t, int e, int size) {
+  const Entry s = entry_of(p, e);
+  SeenBy r;
+  r.q0 = s.q0;
+  r.q_b = s.q_b;
+  r.key0 = t.local ? s.l0 : s.k0;
+  r.len = t.local ? s.m_b : s.k_b;
+  r.lag = t.local ? s.m_b - s.q_b : 0x7fffffff;  // (a nugget: all rows)
+  const int64_t j = t.first - r.key0;           // of the tile's first row
+  r.any = s.q_b > 0 && j < r.len && j + min(t.rows, size) > 0;
+  r.first_row = t.local ? static_cast<int>(max(static_cast<int64_t>(0), max(j, static_cast<int64_t>(0)) - r.lag)) : 0;
+  return r;
+}
+
+// Four consecutive elements from i on as fp32, and the reverse (16 or 8 bytes, aligned to as much).
+template <int DTYPE>
+__device__ __forceinline__ void load4(const void* p, int64_t i, float (&x)[4]) {
+  if (DTYPE == DODO_DTYPE_F32) {
+    const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+    x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
+  }
+}
+template <int DTYPE>
+__device__ __forceinline__ void store4(void* p, int64_t i, float a, float b, float c, float d) {
+  if (DTYPE == DODO_DTYPE_F32)
+    *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(a, b, c, d);
+  else
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+}
+
+}  // namespace dodo

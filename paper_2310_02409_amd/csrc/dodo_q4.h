@@ -1,0 +1,26 @@
+// Nugget caches in 4 bits: what the kernels that write and read them share (the format is described in dodo.h).
+#pragma once
+#include "dodo_common.h"
+
+namespace dodo {
+
+constexpr int kBlockQ4 = 32;          // channels that share a scale
+constexpr uint32_t kScaleBadQ4 = 255;  // scale byte of a block with a NaN or an infinity
+constexpr int kLeastExpQ4 = -125;     // exponents of a scale: no value but 0 is below 2^-126, the least normal number,
+constexpr int kMostExpQ4 = 125;       // and none overflows (6 * 2^125; with 126 a 3.9 would round to 4 * 2^126)
+
+// The scale 2^(byte - 127) as fp32 (bytes 2 .. 254; 255, which stands for NaN, gives infinity here).
+__device__ __forceinline__ float scale_q4(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Eight channels (the codes of 4 bytes, the lowest first) as four pairs of bf16.  The conversion multiplies by the scale's power of
+// two: exact, e2m1 has two bits of mantissa.
+__device__ __forceinline__ uint4 unpack8_bf16(uint32_t codes, float scale) {
+  uint4 v;
+  v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+  v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+  v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+  v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+  return v;
+}
+
+}  // namespace dodo
