@@ -4,12 +4,14 @@
 
 namespace dodo {
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kGradWaves = 4;
 constexpr int kGradThreads = kGradWaves * kWave;
 
 struct GradParams {
-  const void *Q, *Kn, *Vn, *Kl, *Vl, *dO;
-  const float *lse2, *D;  // [H][Sq]
+  const void *Q, *Kn, *Vn, *Kl, *Vl, *dO, *O;
+  const float* lse;
+  float2* stats;  // workspace [H][Sq]: log-sum-exp in base 2, D = dO . O
   const int32_t *cu_q, *cu_nuggets, *cu_local;
   const int32_t *nug_len, *loc_len;  // null: ranges end where the next begins
   int shared;                        // != 0: entries may share rows, so that key tiles run over all rows instead of a sequence's
@@ -78,8 +80,7 @@ __device__ __forceinline__ KeyTile key_tile(const GradParams& p, unsigned item, 
 // Which query rows of an entry see a tile's keys: key j of the entry (of len from row key0 on) is seen by the query rows from
 // max(0, j - lag) on, up to q_b.
 struct SeenBy {
-  int q0, q_b, len, lag, first_row;
-  int64_t key0;
+  int q0, q_b, key0, len, lag, first_row;
   bool any;
   __device__ __forceinline__ int least(int j, bool ok) const { return ok && j >= 0 && j < len ? max(0, j - lag) : 0x7fffffff; }
 };
@@ -97,6 +98,9 @@ __device__ __forceinline__ SeenBy seen_by(const GradParams& p, const KeyTile& t,
   return r;
 }
 
+// bf16, on the bf16 matrix instructions.
+int launch_grad_mfma(const GradParams& p, int32_t d_h);
+
 // Four consecutive elements from i on as fp32, and the reverse (16 or 8 bytes, aligned to as much).
 template <int DTYPE>
 __device__ __forceinline__ void load4(const void* p, int64_t i, float (&x)[4]) {
@@ -108,12 +112,14 @@ __device__ __forceinline__ void load4(const void* p, int64_t i, float (&x)[4]) {
     x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
   }
 }
+typedef __attribute__((ext_vector_type(4))) float floatx4;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 template <int DTYPE>
 __device__ __forceinline__ void store4(void* p, int64_t i, float a, float b, float c, float d) {
   if (DTYPE == DODO_DTYPE_F32)
     *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(a, b, c, d);
   else
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = __builtin_bit_cast(uint2, __builtin_convertvector((floatx4){a, b, c, d}, bf16x4));
 }
 
 }  // namespace dodo

@@ -1,0 +1,493 @@
+// Gradients of nugget attention for bf16 inputs, on the bf16 matrix instructions (the formulas, and why there are two
+// kernels, are in dodo_attn_grad.hip).
+//
+// Both kernels form 32 x 32 blocks of S and dP with v_mfma_f32_32x32x16_bf16 so that a lane owns a row of what the kernel sums (a key,
+// or a query row) and the accumulators run over the rows it walks over.  P and dS, rounded to bf16, are then the right operand of
+// the second product as they stand: accumulator v holds walked row 8 (v / 4) + 4 g + v % 4 (g = lane / 32), and the left operand
+// takes the walked rows in that order.  The walked tile sits in LDS, 64 rows at a time, and is read in two ways: whole rows (16
+// bytes a lane) for S and dP, and columns (transposing reads of 8 bytes) for the second products.  Its 16-byte pieces are
+// swizzled so that both are free of bank conflicts.  The owned rows' fragments and the sums stay in registers.
+#include <type_traits>
+
+#include "dodo_attn_grad.h"
+
+namespace dodo {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) short shortx4;
+typedef __attribute__((ext_vector_type(8))) float floatx8;
+typedef __attribute__((ext_vector_type(16))) float floatx16;
+typedef __attribute__((address_space(3))) void lds_void;
+
+constexpr int kTile = 64;  // walked rows per tile in LDS
+
+template <int DH>
+struct TileDims {
+  static constexpr int kRowBytes = DH * 2;
+  static constexpr int kPieces = kRowBytes / 16;
+  static constexpr int kRowsPerInstr = 64 / kPieces;                       // rows that one direct load brings
+  static constexpr int kInstr = kTile / kRowsPerInstr / kGradWaves;        // direct loads per wavefront, tile and tensor
+  static constexpr int kBytes = kTile * kRowBytes;                         // 16 or 8 KiB
+  // Piece p of row r is stored at p ^ swizzle(r).  A transposing read takes 64-byte granules of 4 rows in a row: these go to
+  // different granules (of a row, or with 128-byte rows of a pair of rows); a row read takes one piece of 8 or 16 rows, which
+  // differ in the granule or inside of it.
+  __device__ static __forceinline__ int swizzle(int r) {
+    return DH == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+  }
+};
+
+// A wavefront's part of the direct loads of a tile of rows `stride` bytes apart: through a buffer that ends with the last
+// valid row (rows beyond read as zeros).
+template <int DH>
+struct TileLoader {
+  using TD = TileDims<DH>;
+  uint32_t voff[TD::kInstr], lds_off;
+  __device__ __forceinline__ void init(int wave, int lane, uint32_t stride) {
+    const int row0 = wave * TD::kInstr * TD::kRowsPerInstr + lane / TD::kPieces, pos = lane % TD::kPieces;
+#pragma unroll
+    for (int u = 0; u < TD::kInstr; ++u) {
+      const int row = row0 + u * TD::kRowsPerInstr;
+      voff[u] = static_cast<uint32_t>(row) * stride + static_cast<uint32_t>(pos ^ TD::swizzle(row)) * 16u;
+    }
+    lds_off = static_cast<uint32_t>(wave) * TD::kInstr * 1024u;
+  }
+  __device__ __forceinline__ void issue(const uint16_t* first, int rows, uint32_t stride, uint32_t lds_dst) const {
+    const u32x4_t buf = buffer_of(first, rows > 0 ? static_cast<uint32_t>(rows - 1) * stride + TD::kRowBytes : 0u);
+#pragma unroll
+    for (int u = 0; u < TD::kInstr; ++u) dma16_buffer(buf, voff[u], __builtin_amdgcn_readfirstlane(lds_dst + lds_off + u * 1024u));
+  }
+};
+
+// One direct load of 4 bytes a lane (lane l's land at lds_dst + 4 l), as dma16_buffer.
+__device__ __forceinline__ void dma4_buffer(const u32x4_t& buf, uint32_t voff, uint32_t lds_dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(buf), "s"(lds_dst) : "memory", "m0");
+}
+
+// Reads of a tile in LDS: fragments of rows and of columns of its 32-row half `hf`.
+template <int DH>
+struct TileReader {
+  using TD = TileDims<DH>;
+  int row_off, row_sw, col_off[2];
+  __device__ __forceinline__ void init(int lane) {
+    const int n = lane & 31, g = lane >> 5;
+    row_off = n * TD::kRowBytes;
+    row_sw = (g ^ TD::swizzle(n)) << 4;
+    const int rr = (lane & 15) >> 2;  // row among 4; 8 bytes at channel 32 cb + 16 (lane / 16 % 2) + 4 (lane % 4)
+    const int low = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = 8 * e + 4 * g + rr;
+      col_off[e] = r * TD::kRowBytes + ((low ^ TD::swizzle(r)) << 4) + 8 * (lane & 1);
+    }
+  }
+  // channels 16 ks + 8 g .. + 8 of row n of the half
+  __device__ __forceinline__ bf16x8 row(const char* tile, int hf, int ks) const {
+    return *reinterpret_cast<const bf16x8*>(tile + hf * 32 * TD::kRowBytes + row_off + (row_sw ^ (ks << 5)));
+  }
+  // channel 32 cb + lane % 32 of rows 16 t + 8 e + 4 g + r of the half (slot 4 e + r)
+  __device__ __forceinline__ bf16x8 column(const char* tile, int hf, int t, int cb) const {
+    shortx4 a[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const char* p = tile + (hf * 32 + 16 * t) * TD::kRowBytes + (col_off[e] ^ (cb << 6));
+      a[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shortx4 __attribute__((address_space(3)))*)(p));
+    }
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+__device__ __forceinline__ floatx16 zero16() {
+  floatx16 z;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) z[v] = 0.f;
+  return z;
+}
+__device__ __forceinline__ floatx16 mfma(const bf16x8& a, const bf16x8& b, const floatx16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// Accumulators 8 t .. 8 t + 7 as a right operand (hardware round-to-nearest-even).
+__device__ __forceinline__ bf16x8 half_bf16(const floatx16& x, int t) {
+  floatx8 h;
+#pragma unroll
+  for (int v = 0; v < 8; ++v) h[v] = x[8 * t + v];
+  return __builtin_convertvector(h, bf16x8);
+}
+
+// Row `off` of a gradient from its transposed blocks: lane (row, g) holds channels 32 cb + 8 v4 + 4 g .. + 4.
+template <int DH>
+__device__ __forceinline__ void store_row(uint16_t* base, int64_t off, int g, const floatx16 (&acc)[DH / 32], float scale) {
+#pragma unroll
+  for (int cb = 0; cb < DH / 32; ++cb)
+#pragma unroll
+    for (int v4 = 0; v4 < 4; ++v4)
+      store4<DODO_DTYPE_BF16>(base, off + 32 * cb + 8 * v4 + 4 * g, acc[cb][4 * v4] * scale, acc[cb][4 * v4 + 1] * scale,
+                              acc[cb][4 * v4 + 2] * scale, acc[cb][4 * v4 + 3] * scale);
+}
+
+// ---- dK, dV ------------------------------------------------------------------------------------------------------------
+// A wavefront owns 32 keys; the workgroup's four walk over the query rows together.
+
+constexpr int kKeys = 32 * kGradWaves;
+
+// A tile of query rows: 64 rows from i0 on of an entry, of head h.
+struct RowTile {
+  int q0, q_b, i0, hg, key0, len, lag;
+  bool valid;
+};
+
+// SHARED: entries may share rows, and those that hold any of the workgroup's keys are looked for, 64 at a time; else the keys are
+// those of one entry.
+template <int DH, bool SHARED>
+__global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, int n_nug_tiles, int n_loc_tiles) {
+  using TD = TileDims<DH>;
+  constexpr int kStage = 2 * TD::kBytes + kTile * 8;  // Q, dO, then (lse2, D) of the rows
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
+  int* const entries = reinterpret_cast<int*>(lds + 2 * kStage);  // (SHARED)
+  // block i runs on XCD i % 8: the key tiles of one (sequence, K/V head) share Q and dO in an XCD's L2
+  const int tiles = n_nug_tiles + n_loc_tiles;
+  const unsigned slot = blockIdx.x >> 3, owner = slot / tiles * 8 + (blockIdx.x & 7);
+  if (owner >= static_cast<unsigned>(p.H_kv * (p.shared ? 1 : p.B))) return;
+  const KeyTile t = key_tile(p, owner * tiles + slot % tiles, n_nug_tiles, n_loc_tiles, kKeys);
+  if (t.rows <= 0) return;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & 31, g = lane >> 5;
+  const int G = p.H / p.H_kv;
+  const int my_rows = min(32, t.rows - wave * 32);  // of this wavefront
+  const bool active = my_rows > 0;
+  const int64_t my_first = t.first + wave * 32;
+
+  const uint32_t row_stride = static_cast<uint32_t>(p.H) * TD::kRowBytes;  // bytes between query rows
+  TileLoader<DH> loader;
+  loader.init(wave, lane, row_stride);
+  TileReader<DH> reader;
+  reader.init(lane);
+
+  // fragments of the owned keys: lane (n, g) holds channels 16 ks + 8 g .. + 8 of key n
+  auto key_offset = [&](int l) { return (t.first + min(wave * 32 + l, t.rows - 1)) * t.tok_stride + t.kvh * t.head_stride; };
+  const int64_t off = key_offset(n);
+  bf16x8 kf[DH / 16], vf[DH / 16];
+#pragma unroll
+  for (int ks = 0; ks < DH / 16; ++ks) {
+    kf[ks] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(t.K) + off + 16 * ks + 8 * g);
+    vf[ks] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(t.V) + off + 16 * ks + 8 * g);
+  }
+  floatx16 dk[DH / 32], dv[DH / 32];
+#pragma unroll
+  for (int cb = 0; cb < DH / 32; ++cb) dk[cb] = dv[cb] = zero16();
+  // (the fragments are used here for the compiler's eyes, so that its waits for them stand before the loop)
+#pragma unroll
+  for (int ks = 0; ks < DH / 16; ++ks) asm volatile("" : "+v"(kf[ks]), "+v"(vf[ks]));
+
+  int e0 = t.entry0;
+  do {
+    RowTile one = {};
+    uint64_t todo = 0;
+    if constexpr (SHARED) {  // (of one entry per lane, kept in LDS: registers are what this kernel is short of)
+      SeenBy of_lane = {};
+      if (e0 + lane < t.entry1) of_lane = seen_by(p, t, e0 + lane, kKeys);
+      todo = __ballot(of_lane.any && of_lane.first_row < of_lane.q_b);
+      __syncthreads();  // (the chunk of entries before this one has been read)
+      if (wave == 0) {
+        entries[lane] = of_lane.q0;
+        entries[kWave + lane] = of_lane.q_b;
+        entries[2 * kWave + lane] = of_lane.len;
+        entries[3 * kWave + lane] = of_lane.lag;
+        entries[4 * kWave + lane] = of_lane.key0;
+        entries[5 * kWave + lane] = of_lane.first_row;
+      }
+      __syncthreads();
+    } else {
+      const SeenBy s = seen_by(p, t, e0, kKeys);
+      todo = s.any && s.first_row < s.q_b;
+      one = RowTile{s.q0, s.q_b, s.first_row, 0, s.key0, s.len, s.lag, todo != 0};
+    }
+    auto entry_tile = [&]() -> RowTile {  // the first tile of the next entry
+      RowTile r = one;
+      r.valid = todo != 0;
+      if (SHARED && r.valid) {
+        const int* of = entries + __ffsll(static_cast<long long>(todo)) - 1;
+        r.q0 = __builtin_amdgcn_readfirstlane(of[0]);
+        r.q_b = __builtin_amdgcn_readfirstlane(of[kWave]);
+        r.len = __builtin_amdgcn_readfirstlane(of[2 * kWave]);
+        r.lag = __builtin_amdgcn_readfirstlane(of[3 * kWave]);
+        r.key0 = __builtin_amdgcn_readfirstlane(of[4 * kWave]);
+        r.i0 = __builtin_amdgcn_readfirstlane(of[5 * kWave]);
+      }
+      todo &= todo - 1;
+      r.i0 = r.i0 / kTile * kTile;
+      r.hg = 0;
+      return r;
+    };
+    auto first_tile = [&](const RowTile& r) {  // of the entry, for the next head
+      return t.local ? static_cast<int>(max(static_cast<int64_t>(0), max(t.first - r.key0, static_cast<int64_t>(0)) - r.lag)) / kTile * kTile : 0;
+    };
+    auto advance = [&](RowTile r) -> RowTile {
+      r.i0 += kTile;
+      if (r.i0 < r.q_b) return r;
+      r.i0 = first_tile(r);
+      if (++r.hg < G) return r;
+      return entry_tile();
+    };
+    auto issue = [&](const RowTile& r, int stage) {
+      const int h = t.kvh * G + r.hg, rows = min(kTile, r.q_b - r.i0);
+      const int64_t first = (static_cast<int64_t>(r.q0 + r.i0) * p.H + h) * DH;
+      const uint32_t dst = lds_base + stage * kStage;
+      loader.issue(static_cast<const uint16_t*>(p.Q) + first, rows, row_stride, dst);
+      loader.issue(static_cast<const uint16_t*>(p.dO) + first, rows, row_stride, dst + TD::kBytes);
+      if (wave < 2) {
+        const u32x4_t buf = buffer_of(p.stats + static_cast<int64_t>(h) * p.Sq + r.q0 + r.i0, rows * 8u);
+        dma4_buffer(buf, wave * 256u + lane * 4u, __builtin_amdgcn_readfirstlane(dst + 2 * TD::kBytes + wave * 256u));
+      }
+    };
+    RowTile cur = entry_tile();
+    if (cur.valid) issue(cur, 0);
+    for (int stage = 0; cur.valid; stage ^= 1) {
+      char* const base = lds + stage * kStage;
+      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wavefront's part of the tile has landed
+      __syncthreads();  // everyone's has, and the other stage has been read
+      const RowTile next = advance(cur);
+      if (next.valid) issue(next, stage ^ 1);
+      // rows [from, ...) see some key of this wavefront; from `all` on they see all of them
+      const int j = static_cast<int>(my_first - cur.key0);
+      int from = 0, all = 0;
+      if (t.local) {
+        from = max(0, max(j, 0) - cur.lag);
+        all = max(0, j + my_rows - 1 - cur.lag);
+      }
+      if (SHARED) {
+        if (j + my_rows <= 0 || j >= cur.len) from = 0x7fffffff;
+        if (j < 0 || j + my_rows > cur.len) all = 0x7fffffff;
+      }
+      if (active) {
+#pragma unroll 1
+        for (int hf = 0; hf < 2; ++hf) {
+          const int i0 = cur.i0 + 32 * hf;
+          if (i0 >= cur.q_b || i0 + 32 <= from) continue;
+          const char *qt = base, *dt = base + TD::kBytes;
+          const char* stats = base + 2 * TD::kBytes + hf * 256 + g * 32;
+          // Fragments are requested one step (two matrix instructions) ahead; the scheduling barriers keep the compiler from
+          // requesting them all at once, which would not fit into the registers.
+          floatx16 s = zero16(), dp = zero16();
+          bf16x8 qa[2], da[2];
+          qa[0] = reader.row(qt, hf, 0);
+          da[0] = reader.row(dt, hf, 0);
+#pragma unroll
+          for (int ks = 0; ks < DH / 16; ++ks) {
+            if (ks + 1 < DH / 16) {
+              qa[(ks + 1) & 1] = reader.row(qt, hf, ks + 1);
+              da[(ks + 1) & 1] = reader.row(dt, hf, ks + 1);
+            }
+            s = mfma(qa[ks & 1], kf[ks], s);
+            dp = mfma(da[ks & 1], vf[ks], dp);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          // weights and dS; rows past the entry's last one are zeros with log-sum-exp 0 and D 0: they add nothing
+          const bool mask = i0 < all;
+#pragma unroll
+          for (int v4 = 0; v4 < 4; ++v4) {
+            const float4 a = *reinterpret_cast<const float4*>(stats + 64 * v4), b = *reinterpret_cast<const float4*>(stats + 64 * v4 + 16);
+            const float lse2[4] = {a.x, a.z, b.x, b.z}, D[4] = {a.y, a.w, b.y, b.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int v = 4 * v4 + r;
+              s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], p.scale_log2e, -lse2[r]));
+              dp[v] = s[v] * (dp[v] - D[r]);
+            }
+          }
+          if (mask) {
+            const int jk = j + n;
+            int least = t.local ? jk - cur.lag : 0;
+            if (SHARED && (jk < 0 || jk >= cur.len)) least = 0x7fffffff;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+              const bool seen = i0 + 8 * (v >> 2) + 4 * g + (v & 3) >= least;
+              s[v] = seen ? s[v] : 0.f;
+              dp[v] = seen ? dp[v] : 0.f;
+            }
+          }
+          const bf16x8 pf[2] = {half_bf16(s, 0), half_bf16(s, 1)}, sf[2] = {half_bf16(dp, 0), half_bf16(dp, 1)};
+          constexpr int kCB = DH / 32;
+          bf16x8 dc[2], qc[2];
+          dc[0] = reader.column(dt, hf, 0, 0);
+          qc[0] = reader.column(qt, hf, 0, 0);
+#pragma unroll
+          for (int u = 0; u < 2 * kCB; ++u) {
+            if (u + 1 < 2 * kCB) {
+              dc[(u + 1) & 1] = reader.column(dt, hf, (u + 1) / kCB, (u + 1) % kCB);
+              qc[(u + 1) & 1] = reader.column(qt, hf, (u + 1) / kCB, (u + 1) % kCB);
+            }
+            dv[u % kCB] = mfma(dc[u & 1], pf[u / kCB], dv[u % kCB]);
+            dk[u % kCB] = mfma(qc[u & 1], sf[u / kCB], dk[u % kCB]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      cur = next;
+    }
+    e0 += kWave;
+  } while (SHARED && e0 < t.entry1);
+  int l = n;
+  asm volatile("" : "+v"(l));  // (made again here: held through the loop, the offset's registers would be missing there)
+  if (l >= my_rows) return;
+  store_row<DH>(static_cast<uint16_t*>(t.dK), key_offset(l), g, dk, p.scale);
+  store_row<DH>(static_cast<uint16_t*>(t.dV), key_offset(l), g, dv, 1.f);
+}
+
+// ---- dQ ----------------------------------------------------------------------------------------------------------------
+// A wavefront owns 32 query rows of a head; the workgroup's four walk over the keys together: nuggets, then local rows up to the
+// last one that the workgroup's last row sees.
+constexpr int kQueryRows = 32 * kGradWaves;
+
+template <int DH>
+__global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, int n_blocks) {
+  using TD = TileDims<DH>;
+  constexpr int kStage = 2 * TD::kBytes;  // K, V
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
+  const unsigned slot = blockIdx.x >> 3, owner = slot / n_blocks * 8 + (blockIdx.x & 7);
+  if (owner >= static_cast<unsigned>(p.H * p.B)) return;
+  const int h = owner % p.H;
+  const Entry s = entry_of(p, owner / p.H);
+  const int i0 = static_cast<int>(n_blocks - 1 - slot % n_blocks) * kQueryRows;  // the last rows see the most keys: they start first
+  if (i0 >= s.q_b) return;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & 31, g = lane >> 5;
+  const int kvh = h / (p.H / p.H_kv);
+  const int w_i0 = i0 + 32 * wave;
+  const bool active = w_i0 < s.q_b, row_ok = w_i0 + n < s.q_b;
+  const int i = min(w_i0 + n, s.q_b - 1);
+  const int64_t off = (static_cast<int64_t>(s.q0 + i) * p.H + h) * DH;
+  TileLoader<DH> loader;
+  uint32_t loader_stride = 0;
+  TileReader<DH> reader;
+  reader.init(lane);
+  const int lag = s.m_b - s.q_b + 1;  // row i sees local rows [0, i + lag)
+  const int vis = max(0, min(s.m_b, i + lag));
+  const int w_least = max(0, min(s.m_b, w_i0 + lag)), w_most = max(0, min(s.m_b, min(w_i0 + 32, s.q_b) - 1 + lag));
+  const int wg_most = max(0, min(s.m_b, min(i0 + kQueryRows, s.q_b) - 1 + lag));
+  const int n_nug = (s.k_b + kTile - 1) / kTile, n_tiles = n_nug + (wg_most + kTile - 1) / kTile;
+  const int64_t nug_first = s.k0 * p.nug_tok_stride + kvh * p.nug_head_stride, loc_first = s.l0 * p.loc_tok_stride + kvh * p.loc_head_stride;
+  auto issue = [&](int tile, int stage) {
+    const bool nug = tile < n_nug;
+    const int j0 = kTile * (nug ? tile : tile - n_nug), rows = min(kTile, (nug ? s.k_b : wg_most) - j0);
+    const int64_t stride = nug ? p.nug_tok_stride : p.loc_tok_stride, first = (nug ? nug_first : loc_first) + j0 * stride;
+    const uint32_t dst = lds_base + stage * kStage;
+    if (loader_stride != static_cast<uint32_t>(stride * 2)) {  // (the first tile, and where the cache's stride is not the local rows')
+      loader_stride = static_cast<uint32_t>(stride * 2);
+      loader.init(wave, lane, loader_stride);
+    }
+    loader.issue(static_cast<const uint16_t*>(nug ? p.Kn : p.Kl) + first, rows, loader_stride, dst);
+    loader.issue(static_cast<const uint16_t*>(nug ? p.Vn : p.Vl) + first, rows, loader_stride, dst + TD::kBytes);
+  };
+  bf16x8 qf[DH / 16], df[DH / 16];
+#pragma unroll
+  for (int ks = 0; ks < DH / 16; ++ks) {
+    qf[ks] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.Q) + off + 16 * ks + 8 * g);
+    df[ks] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.dO) + off + 16 * ks + 8 * g);
+  }
+  // D and the log-sum-exp in base 2 of the row, here and for the other kernel; a row that sees nothing (-inf) gets +inf: its
+  // weights are 0
+  float2 st = make_float2(p.lse[static_cast<int64_t>(s.q0 + i) * p.H + h] * kLog2e, 0.f);
+  if (st.x == -__builtin_inff()) st.x = __builtin_inff();
+#pragma unroll
+  for (int ks = 0; ks < DH / 16; ++ks) {
+    const uint4 a = __builtin_bit_cast(uint4, df[ks]), o = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.O) + off + 16 * ks + 8 * g);
+    const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, ow[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      st.y = fmaf(bf16_lo(aw[c]), bf16_lo(ow[c]), st.y);
+      st.y = fmaf(bf16_hi(aw[c]), bf16_hi(ow[c]), st.y);
+    }
+  }
+  float lower, upper;
+  lane_pair<32>(st.y, lower, upper);
+  st.y = lower + upper;
+  if (g == 0 && row_ok) p.stats[static_cast<int64_t>(h) * p.Sq + s.q0 + i] = st;
+  floatx16 dq[DH / 32];
+#pragma unroll
+  for (int cb = 0; cb < DH / 32; ++cb) dq[cb] = zero16();
+#pragma unroll
+  for (int ks = 0; ks < DH / 16; ++ks) asm volatile("" : "+v"(qf[ks]), "+v"(df[ks]));
+  asm volatile("" : "+v"(st.x), "+v"(st.y));
+  if (n_tiles > 0) issue(0, 0);
+  for (int tile = 0; tile < n_tiles; ++tile) {
+    const int stage = tile & 1;
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wavefront's part of the tile has landed
+    __syncthreads();                      // everyone's has, and the other stage has been read
+    if (tile + 1 < n_tiles) issue(tile + 1, stage ^ 1);
+    if (!active) continue;
+    const bool nug = tile < n_nug;
+    const int j0 = kTile * (nug ? tile : tile - n_nug);
+    const int limit = (nug ? s.k_b : vis) - j0;  // keys [0, limit) of the tile are seen by this lane's row,
+    const int most = (nug ? s.k_b : w_most) - j0, least = (nug ? s.k_b : w_least) - j0;  // ... by some and by all rows of the wavefront
+    const char *kt = lds + stage * kStage, *vt = kt + TD::kBytes;
+#pragma unroll 1
+    for (int hf = 0; hf < 2; ++hf) {
+      if (32 * hf >= most) break;
+      floatx16 sc = zero16(), dp = zero16();
+#pragma unroll
+      for (int ks = 0; ks < DH / 16; ++ks) {
+        sc = mfma(reader.row(kt, hf, ks), qf[ks], sc);
+        dp = mfma(reader.row(vt, hf, ks), df[ks], dp);
+      }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], p.scale_log2e, -st.x)) * (dp[v] - st.y);
+      if (32 * hf + 32 > least) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sc[v] = 32 * hf + 8 * (v >> 2) + 4 * g + (v & 3) < limit ? sc[v] : 0.f;
+      }
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const bf16x8 sf = half_bf16(sc, tt);
+#pragma unroll
+        for (int cb = 0; cb < DH / 32; ++cb) dq[cb] = mfma(reader.column(kt, hf, tt, cb), sf, dq[cb]);
+      }
+    }
+  }
+  if (row_ok) store_row<DH>(static_cast<uint16_t*>(p.dQ), off, g, dq, p.scale);
+}
+
+template <int DH, bool SHARED>
+int launch_kv(const GradParams& p) {
+  constexpr int kLds = 2 * (2 * TileDims<DH>::kBytes + kTile * 8) + (SHARED ? 6 * kWave * 4 : 0);
+  const int64_t nug_rows = p.shared ? p.Kt : p.max_k, loc_rows = p.shared ? p.Sm : p.max_local;
+  const int64_t nug = (nug_rows + kKeys - 1) / kKeys, loc = (loc_rows + kKeys - 1) / kKeys;
+  const int64_t owners = (static_cast<int64_t>(p.H_kv) * (p.shared ? 1 : p.B) + 7) / 8 * 8;
+  if ((nug + loc) * owners > 0x7fffffffLL) return DODO_ERR_UNSUPPORTED;
+  if (nug + loc == 0) return DODO_OK;
+  const auto kern = grad_kv_kernel<DH, SHARED>;
+  const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kern), kLds);
+  if (rc != DODO_OK) return rc;
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((nug + loc) * owners)), dim3(kGradThreads), kLds, p.stream, p, static_cast<int>(nug),
+                     static_cast<int>(loc));
+  return launch_status();
+}
+
+template <int DH>
+int launch_q(const GradParams& p) {
+  constexpr int kLds = 2 * 2 * TileDims<DH>::kBytes;
+  const int64_t blocks = (static_cast<int64_t>(p.max_q) + kQueryRows - 1) / kQueryRows;
+  const int64_t owners = (static_cast<int64_t>(p.H) * p.B + 7) / 8 * 8;
+  if (blocks * owners > 0x7fffffffLL) return DODO_ERR_UNSUPPORTED;
+  if (blocks * owners == 0) return DODO_OK;
+  const auto kern = grad_q_kernel<DH>;
+  const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kern), kLds);
+  if (rc != DODO_OK) return rc;
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks * owners)), dim3(kGradThreads), kLds, p.stream, p, static_cast<int>(blocks));
+  return launch_status();
+}
+
+template <int DH>
+int launch_both(const GradParams& p) {
+  const int rc = launch_q<DH>(p);  // (first: it makes the rows' statistics)
+  if (rc != DODO_OK) return rc;
+  return p.shared ? launch_kv<DH, true>(p) : launch_kv<DH, false>(p);
+}
+
+}  // namespace
+
+int launch_grad_mfma(const GradParams& p, int32_t d_h) {
+  return d_h == 128 ? launch_both<128>(p) : launch_both<64>(p);
+}
+
+}  // namespace dodo
