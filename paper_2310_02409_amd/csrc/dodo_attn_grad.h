@@ -11,7 +11,7 @@ constexpr int kGradThreads = kGradWaves * kWave;
 struct GradParams {
   const void *Q, *Kn, *Vn, *Kl, *Vl, *dO, *O;
   const float* lse;
-  float2* stats;  // workspace [H][Sq]: log-sum-exp in base 2, D = dO . O
+  float *lse2, *neg_d;  // workspace [H][Sq]: log-sum-exp in base 2, -D = -dO . O
   const int32_t *cu_q, *cu_nuggets, *cu_local;
   const int32_t *nug_len, *loc_len;  // null: ranges end where the next begins
   int shared;                        // != 0: entries may share rows, so that key tiles run over all rows instead of a sequence's

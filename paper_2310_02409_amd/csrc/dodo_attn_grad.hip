@@ -14,11 +14,11 @@ namespace {
 
 typedef __attribute__((ext_vector_type(16))) float floatx16;
 
-// stats[h][row] = (lse[row,h] * log2(e), D = dO[row,h] . O[row,h]), by heads, so that the rows of a head lie side by side.
+// lse2[h][row] = lse[row,h] * log2(e) and neg_d[h][row] = -dO[row,h] . O[row,h], by heads, so that the rows of a head lie side by side.
 // A row that sees nothing (lse = -inf) gets +inf: its weights are 0.  16 lanes per (row, head).
 __global__ __launch_bounds__(256) void grad_rows_kernel(const float* __restrict__ dO, const float* __restrict__ O,
                                                         const float* __restrict__ lse, int64_t Sq, int H, int d_h,
-                                                        float2* __restrict__ stats) {
+                                                        float* __restrict__ lse2, float* __restrict__ neg_d) {
   const int64_t t = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / 16;
   if (t >= Sq * H) return;
   const int sub = threadIdx.x % 16;
@@ -30,7 +30,8 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(const float* __restrict_
   acc = lanes_sum<16>(acc);
   if (sub == 0) {
     const float l = lse[t];
-    stats[(t % H) * Sq + t / H] = make_float2(l == -__builtin_inff() ? __builtin_inff() : l * kLog2e, acc);
+    lse2[(t % H) * Sq + t / H] = l == -__builtin_inff() ? __builtin_inff() : l * kLog2e;
+    neg_d[(t % H) * Sq + t / H] = -acc;
   }
 }
 
@@ -138,10 +139,9 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_kv_plain_kernel(GradPara
         for (int v = 0; v < 16; ++v) {
           const int i = i0 + 8 * (v >> 2) + 4 * g + (v & 3), ic = min(i, s.q_b - 1);
           const bool vis = i >= least && i < s.q_b;
-          const float2 st = p.stats[stat + ic];
-          const float w = __builtin_amdgcn_exp2f(ds[v] * p.scale_log2e - st.x);
+          const float w = __builtin_amdgcn_exp2f(ds[v] * p.scale_log2e - p.lse2[stat + ic]);
           pr[v] = vis ? w : 0.f;
-          ds[v] = vis ? w * (dp[v] - st.y) : 0.f;
+          ds[v] = vis ? w * (dp[v] + p.neg_d[stat + ic]) : 0.f;
         }
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_q_plain_kernel(GradParam
   float qf[DH / 2], df[DH / 2];
   load_row<DH>(p.Q, off + 4 * g, qf);
   load_row<DH>(p.dO, off + 4 * g, df);
-  const float2 st = p.stats[static_cast<int64_t>(h) * p.Sq + s.q0 + i];
+  const float lse2 = p.lse2[static_cast<int64_t>(h) * p.Sq + s.q0 + i], neg_d = p.neg_d[static_cast<int64_t>(h) * p.Sq + s.q0 + i];
   const int kvh = h / (p.H / p.H_kv);
   const int vis = max(0, min(s.m_b, s.m_b - s.q_b + i + 1));  // local rows that this lane's row sees
   const int most = max(0, min(s.m_b, s.m_b - s.q_b + min(i0 + 32, s.q_b)));
@@ -195,8 +195,8 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_q_plain_kernel(GradParam
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int j = j0 + 8 * (v >> 2) + 4 * g + (v & 3);
-      const float w = __builtin_amdgcn_exp2f(ds[v] * p.scale_log2e - st.x);
-      ds[v] = j < seen ? w * (dp[v] - st.y) : 0.f;
+      const float w = __builtin_amdgcn_exp2f(ds[v] * p.scale_log2e - lse2);
+      ds[v] = j < seen ? w * (dp[v] + neg_d) : 0.f;
     }
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
@@ -260,11 +260,12 @@ int grad_entry(GradParams& p, int32_t d_h, int dtype, int layout, void* ws, size
   p.loc_tok_stride = static_cast<int64_t>(p.H_kv) * d_h;
   p.loc_head_stride = d_h;
   p.scale_log2e = p.scale * kLog2e;
-  p.stats = static_cast<float2*>(ws);
+  p.lse2 = static_cast<float*>(ws);
+  p.neg_d = p.lse2 + p.Sq * p.H;
   if (dtype == DODO_DTYPE_BF16) return launch_grad_mfma(p, d_h);
   if (p.max_q > 0) {
     hipLaunchKernelGGL(grad_rows_kernel, dim3(static_cast<unsigned>((p.Sq * p.H * 16 + 255) / 256)), dim3(256), 0, p.stream,
-                       static_cast<const float*>(p.dO), static_cast<const float*>(p.O), p.lse, p.Sq, p.H, d_h, p.stats);
+                       static_cast<const float*>(p.dO), static_cast<const float*>(p.O), p.lse, p.Sq, p.H, d_h, p.lse2, p.neg_d);
     const int rc = launch_status();
     if (rc != DODO_OK) return rc;
   }

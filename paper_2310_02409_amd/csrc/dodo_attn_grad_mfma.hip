@@ -27,7 +27,6 @@ struct TileDims {
   static constexpr int kRowBytes = DH * 2;
   static constexpr int kPieces = kRowBytes / 16;
   static constexpr int kRowsPerInstr = 64 / kPieces;                       // rows that one direct load brings
-  static constexpr int kInstr = kTile / kRowsPerInstr / kGradWaves;        // direct loads per wavefront, tile and tensor
   static constexpr int kBytes = kTile * kRowBytes;                         // 16 or 8 KiB
   // Piece p of row r is stored at p ^ swizzle(r).  A transposing read takes 64-byte granules of 4 rows in a row: these go to
   // different granules (of a row, or with 128-byte rows of a pair of rows); a row read takes one piece of 8 or 16 rows, which
@@ -39,23 +38,25 @@ struct TileDims {
 
 // A wavefront's part of the direct loads of a tile of rows `stride` bytes apart: through a buffer that ends with the last
 // valid row (rows beyond read as zeros).
-template <int DH>
+template <int DH, int NW>
 struct TileLoader {
   using TD = TileDims<DH>;
-  uint32_t voff[TD::kInstr], lds_off;
+  static constexpr int kInstr = kTile / TD::kRowsPerInstr / NW;  // direct loads per wavefront, tile and tensor
+  static_assert(kInstr > 0, "every wavefront brings part of a tile");
+  uint32_t voff[kInstr], lds_off;
   __device__ __forceinline__ void init(int wave, int lane, uint32_t stride) {
-    const int row0 = wave * TD::kInstr * TD::kRowsPerInstr + lane / TD::kPieces, pos = lane % TD::kPieces;
+    const int row0 = wave * kInstr * TD::kRowsPerInstr + lane / TD::kPieces, pos = lane % TD::kPieces;
 #pragma unroll
-    for (int u = 0; u < TD::kInstr; ++u) {
+    for (int u = 0; u < kInstr; ++u) {
       const int row = row0 + u * TD::kRowsPerInstr;
       voff[u] = static_cast<uint32_t>(row) * stride + static_cast<uint32_t>(pos ^ TD::swizzle(row)) * 16u;
     }
-    lds_off = static_cast<uint32_t>(wave) * TD::kInstr * 1024u;
+    lds_off = static_cast<uint32_t>(wave) * kInstr * 1024u;
   }
   __device__ __forceinline__ void issue(const uint16_t* first, int rows, uint32_t stride, uint32_t lds_dst) const {
     const u32x4_t buf = buffer_of(first, rows > 0 ? static_cast<uint32_t>(rows - 1) * stride + TD::kRowBytes : 0u);
 #pragma unroll
-    for (int u = 0; u < TD::kInstr; ++u) dma16_buffer(buf, voff[u], __builtin_amdgcn_readfirstlane(lds_dst + lds_off + u * 1024u));
+    for (int u = 0; u < kInstr; ++u) dma16_buffer(buf, voff[u], __builtin_amdgcn_readfirstlane(lds_dst + lds_off + u * 1024u));
   }
 };
 
@@ -126,7 +127,8 @@ __device__ __forceinline__ void store_row(uint16_t* base, int64_t off, int g, co
 }
 
 // ---- dK, dV ------------------------------------------------------------------------------------------------------------
-// A wavefront owns 32 keys; the workgroup's four walk over the query rows together.
+// A wavefront owns 32 keys, a workgroup 128; its wavefronts walk over the query rows together.  PARTS = 2: eight wavefronts, two per 32
+// keys, one for either half of a tile's rows, whose sums meet in LDS at the end.
 
 constexpr int kKeys = 32 * kGradWaves;
 
@@ -138,33 +140,36 @@ struct RowTile {
 
 // SHARED: entries may share rows, and those that hold any of the workgroup's keys are looked for, 64 at a time; else the keys are
 // those of one entry.
-template <int DH, bool SHARED>
-__global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, int n_nug_tiles, int n_loc_tiles) {
+template <int DH, int PARTS, bool SHARED>
+__global__ __launch_bounds__(PARTS * kGradThreads, PARTS == 1 ? 2 : 1) void grad_kv_kernel(GradParams p, int n_nug_tiles, int n_loc_tiles) {
   using TD = TileDims<DH>;
-  constexpr int kStage = 2 * TD::kBytes + kTile * 8;  // Q, dO, then (lse2, D) of the rows
+  constexpr int kStage = 2 * TD::kBytes + kTile * 8;  // Q, dO, then log-sum-exp (base 2) and -D of the rows
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
   int* const entries = reinterpret_cast<int*>(lds + 2 * kStage);  // (SHARED)
-  // block i runs on XCD i % 8: the key tiles of one (sequence, K/V head) share Q and dO in an XCD's L2
-  const int tiles = n_nug_tiles + n_loc_tiles;
-  const unsigned slot = blockIdx.x >> 3, owner = slot / tiles * 8 + (blockIdx.x & 7);
-  if (owner >= static_cast<unsigned>(p.H_kv * (p.shared ? 1 : p.B))) return;
-  const KeyTile t = key_tile(p, owner * tiles + slot % tiles, n_nug_tiles, n_loc_tiles, kKeys);
+  // block i runs on XCD i % 8: the key tiles of one (sequence, K/V head) share Q and dO in an XCD's L2.  Shared rows: tile by
+  // tile instead, so that the nuggets, which most entries see, come first for every head.
+  const int tiles = n_nug_tiles + n_loc_tiles, n_owners = p.H_kv * (SHARED ? 1 : p.B), by_xcd = (n_owners + 7) / 8;
+  const unsigned slot = blockIdx.x >> 3;
+  const unsigned owner = (SHARED ? slot % by_xcd : slot / tiles) * 8 + (blockIdx.x & 7), tile = SHARED ? slot / by_xcd : slot % tiles;
+  if (owner >= static_cast<unsigned>(n_owners)) return;
+  const KeyTile t = key_tile(p, owner * tiles + tile, n_nug_tiles, n_loc_tiles, kKeys);
   if (t.rows <= 0) return;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & 31, g = lane >> 5;
   const int G = p.H / p.H_kv;
-  const int my_rows = min(32, t.rows - wave * 32);  // of this wavefront
+  const int blk = wave % kGradWaves, part = wave / kGradWaves;
+  const int my_rows = min(32, t.rows - blk * 32);  // of this wavefront
   const bool active = my_rows > 0;
-  const int64_t my_first = t.first + wave * 32;
+  const int64_t my_first = t.first + blk * 32;
 
   const uint32_t row_stride = static_cast<uint32_t>(p.H) * TD::kRowBytes;  // bytes between query rows
-  TileLoader<DH> loader;
+  TileLoader<DH, PARTS * kGradWaves> loader;
   loader.init(wave, lane, row_stride);
   TileReader<DH> reader;
   reader.init(lane);
 
   // fragments of the owned keys: lane (n, g) holds channels 16 ks + 8 g .. + 8 of key n
-  auto key_offset = [&](int l) { return (t.first + min(wave * 32 + l, t.rows - 1)) * t.tok_stride + t.kvh * t.head_stride; };
+  auto key_offset = [&](int l) { return (t.first + min(blk * 32 + l, t.rows - 1)) * t.tok_stride + t.kvh * t.head_stride; };
   const int64_t off = key_offset(n);
   bf16x8 kf[DH / 16], vf[DH / 16];
 #pragma unroll
@@ -236,8 +241,8 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, 
       loader.issue(static_cast<const uint16_t*>(p.Q) + first, rows, row_stride, dst);
       loader.issue(static_cast<const uint16_t*>(p.dO) + first, rows, row_stride, dst + TD::kBytes);
       if (wave < 2) {
-        const u32x4_t buf = buffer_of(p.stats + static_cast<int64_t>(h) * p.Sq + r.q0 + r.i0, rows * 8u);
-        dma4_buffer(buf, wave * 256u + lane * 4u, __builtin_amdgcn_readfirstlane(dst + 2 * TD::kBytes + wave * 256u));
+        const float* from = (wave == 0 ? p.lse2 : p.neg_d) + static_cast<int64_t>(h) * p.Sq + r.q0 + r.i0;
+        dma4_buffer(buffer_of(from, rows * 4u), lane * 4u, __builtin_amdgcn_readfirstlane(dst + 2 * TD::kBytes + wave * (kTile * 4)));
       }
     };
     RowTile cur = entry_tile();
@@ -261,14 +266,19 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, 
       }
       if (active) {
 #pragma unroll 1
-        for (int hf = 0; hf < 2; ++hf) {
+        for (int hf = part; hf < 2; hf += PARTS) {
           const int i0 = cur.i0 + 32 * hf;
           if (i0 >= cur.q_b || i0 + 32 <= from) continue;
           const char *qt = base, *dt = base + TD::kBytes;
-          const char* stats = base + 2 * TD::kBytes + hf * 256 + g * 32;
+          const float* lse2 = reinterpret_cast<const float*>(base + 2 * TD::kBytes) + 32 * hf + 4 * g;
           // Fragments are requested one step (two matrix instructions) ahead; the scheduling barriers keep the compiler from
           // requesting them all at once, which would not fit into the registers.
-          floatx16 s = zero16(), dp = zero16();
+          floatx16 s = zero16(), dp;  // (dP starts from -D, which saves the subtractions)
+#pragma unroll
+          for (int v4 = 0; v4 < 4; ++v4) {
+            const float4 d = *reinterpret_cast<const float4*>(lse2 + kTile + 8 * v4);
+            dp[4 * v4] = d.x; dp[4 * v4 + 1] = d.y; dp[4 * v4 + 2] = d.z; dp[4 * v4 + 3] = d.w;
+          }
           bf16x8 qa[2], da[2];
           qa[0] = reader.row(qt, hf, 0);
           da[0] = reader.row(dt, hf, 0);
@@ -286,13 +296,13 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, 
           const bool mask = i0 < all;
 #pragma unroll
           for (int v4 = 0; v4 < 4; ++v4) {
-            const float4 a = *reinterpret_cast<const float4*>(stats + 64 * v4), b = *reinterpret_cast<const float4*>(stats + 64 * v4 + 16);
-            const float lse2[4] = {a.x, a.z, b.x, b.z}, D[4] = {a.y, a.w, b.y, b.w};
+            const float4 l = *reinterpret_cast<const float4*>(lse2 + 8 * v4);
+            const float lv[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int v = 4 * v4 + r;
-              s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], p.scale_log2e, -lse2[r]));
-              dp[v] = s[v] * (dp[v] - D[r]);
+              s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], p.scale_log2e, -lv[r]));
+              dp[v] *= s[v];
             }
           }
           if (mask) {
@@ -307,18 +317,19 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, 
             }
           }
           const bf16x8 pf[2] = {half_bf16(s, 0), half_bf16(s, 1)}, sf[2] = {half_bf16(dp, 0), half_bf16(dp, 1)};
-          constexpr int kCB = DH / 32;
-          bf16x8 dc[2], qc[2];
-          dc[0] = reader.column(dt, hf, 0, 0);
-          qc[0] = reader.column(qt, hf, 0, 0);
+          constexpr int kCB = DH / 32, kAhead = 2;
+          bf16x8 dc[kAhead + 1], qc[kAhead + 1];
+          const auto read = [&](int u) {
+            dc[u % (kAhead + 1)] = reader.column(dt, hf, u / kCB, u % kCB);
+            qc[u % (kAhead + 1)] = reader.column(qt, hf, u / kCB, u % kCB);
+          };
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) read(u);
 #pragma unroll
           for (int u = 0; u < 2 * kCB; ++u) {
-            if (u + 1 < 2 * kCB) {
-              dc[(u + 1) & 1] = reader.column(dt, hf, (u + 1) / kCB, (u + 1) % kCB);
-              qc[(u + 1) & 1] = reader.column(qt, hf, (u + 1) / kCB, (u + 1) % kCB);
-            }
-            dv[u % kCB] = mfma(dc[u & 1], pf[u / kCB], dv[u % kCB]);
-            dk[u % kCB] = mfma(qc[u & 1], sf[u / kCB], dk[u % kCB]);
+            if (u + kAhead < 2 * kCB) read(u + kAhead);
+            dv[u % kCB] = mfma(dc[u % (kAhead + 1)], pf[u / kCB], dv[u % kCB]);
+            dk[u % kCB] = mfma(qc[u % (kAhead + 1)], sf[u / kCB], dk[u % kCB]);
             __builtin_amdgcn_sched_barrier(0);
           }
         }
@@ -327,6 +338,24 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, 
     }
     e0 += kWave;
   } while (SHARED && e0 < t.entry1);
+  if constexpr (PARTS == 2) {
+    constexpr int kRegs = DH / 32 * 16;  // per lane and tensor
+    float* meet = reinterpret_cast<float*>(lds) + blk * 2 * kRegs * kWave + lane;
+    __syncthreads();  // the stages have been read
+    if (part == 1)
+#pragma unroll
+      for (int c = 0; c < kRegs; ++c) {
+        meet[c * kWave] = dk[c / 16][c % 16];
+        meet[(kRegs + c) * kWave] = dv[c / 16][c % 16];
+      }
+    __syncthreads();
+    if (part == 1) return;
+#pragma unroll
+    for (int c = 0; c < kRegs; ++c) {
+      dk[c / 16][c % 16] += meet[c * kWave];
+      dv[c / 16][c % 16] += meet[(kRegs + c) * kWave];
+    }
+  }
   int l = n;
   asm volatile("" : "+v"(l));  // (made again here: held through the loop, the offset's registers would be missing there)
   if (l >= my_rows) return;
@@ -343,6 +372,7 @@ template <int DH>
 __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, int n_blocks) {
   using TD = TileDims<DH>;
   constexpr int kStage = 2 * TD::kBytes;  // K, V
+  constexpr int kAhead = 2;               // steps that fragments are requested ahead
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
   const unsigned slot = blockIdx.x >> 3, owner = slot / n_blocks * 8 + (blockIdx.x & 7);
@@ -357,7 +387,7 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
   const bool active = w_i0 < s.q_b, row_ok = w_i0 + n < s.q_b;
   const int i = min(w_i0 + n, s.q_b - 1);
   const int64_t off = (static_cast<int64_t>(s.q0 + i) * p.H + h) * DH;
-  TileLoader<DH> loader;
+  TileLoader<DH, kGradWaves> loader;
   uint32_t loader_stride = 0;
   TileReader<DH> reader;
   reader.init(lane);
@@ -379,6 +409,7 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
     loader.issue(static_cast<const uint16_t*>(nug ? p.Kn : p.Kl) + first, rows, loader_stride, dst);
     loader.issue(static_cast<const uint16_t*>(nug ? p.Vn : p.Vl) + first, rows, loader_stride, dst + TD::kBytes);
   };
+  if (n_tiles > 0) issue(0, 0);
   bf16x8 qf[DH / 16], df[DH / 16];
 #pragma unroll
   for (int ks = 0; ks < DH / 16; ++ks) {
@@ -401,15 +432,20 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
   }
   float lower, upper;
   lane_pair<32>(st.y, lower, upper);
-  st.y = lower + upper;
-  if (g == 0 && row_ok) p.stats[static_cast<int64_t>(h) * p.Sq + s.q0 + i] = st;
+  st.y = -(lower + upper);
+  if (g == 0 && row_ok) {
+    p.lse2[static_cast<int64_t>(h) * p.Sq + s.q0 + i] = st.x;
+    p.neg_d[static_cast<int64_t>(h) * p.Sq + s.q0 + i] = st.y;
+  }
+  floatx16 neg_d;  // dP starts from -D, which saves the subtractions
+#pragma unroll
+  for (int v = 0; v < 16; ++v) neg_d[v] = st.y;
   floatx16 dq[DH / 32];
 #pragma unroll
   for (int cb = 0; cb < DH / 32; ++cb) dq[cb] = zero16();
 #pragma unroll
   for (int ks = 0; ks < DH / 16; ++ks) asm volatile("" : "+v"(qf[ks]), "+v"(df[ks]));
   asm volatile("" : "+v"(st.x), "+v"(st.y));
-  if (n_tiles > 0) issue(0, 0);
   for (int tile = 0; tile < n_tiles; ++tile) {
     const int stage = tile & 1;
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wavefront's part of the tile has landed
@@ -424,41 +460,69 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
 #pragma unroll 1
     for (int hf = 0; hf < 2; ++hf) {
       if (32 * hf >= most) break;
-      floatx16 sc = zero16(), dp = zero16();
+      floatx16 sc = zero16(), dp = neg_d;
+      {
+        bf16x8 ka[kAhead + 1], va[kAhead + 1];
+        const auto read = [&](int ks) {
+          ka[ks % (kAhead + 1)] = reader.row(kt, hf, ks);
+          va[ks % (kAhead + 1)] = reader.row(vt, hf, ks);
+        };
 #pragma unroll
-      for (int ks = 0; ks < DH / 16; ++ks) {
-        sc = mfma(reader.row(kt, hf, ks), qf[ks], sc);
-        dp = mfma(reader.row(vt, hf, ks), df[ks], dp);
+        for (int ks = 0; ks < kAhead; ++ks) read(ks);
+#pragma unroll
+        for (int ks = 0; ks < DH / 16; ++ks) {
+          if (ks + kAhead < DH / 16) read(ks + kAhead);
+          sc = mfma(ka[ks % (kAhead + 1)], qf[ks], sc);
+          dp = mfma(va[ks % (kAhead + 1)], df[ks], dp);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
+      constexpr int kCB = DH / 32;
+      bf16x8 kc[2 * kAhead];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], p.scale_log2e, -st.x)) * (dp[v] - st.y);
+      for (int u = 0; u < 2 * kAhead - 1; ++u) kc[u] = reader.column(kt, hf, u / kCB, u % kCB);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sc[v] = __builtin_amdgcn_exp2f(fmaf(sc[v], p.scale_log2e, -st.x)) * dp[v];
       if (32 * hf + 32 > least) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) sc[v] = 32 * hf + 8 * (v >> 2) + 4 * g + (v & 3) < limit ? sc[v] : 0.f;
       }
+      const bf16x8 sf[2] = {half_bf16(sc, 0), half_bf16(sc, 1)};
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const bf16x8 sf = half_bf16(sc, tt);
-#pragma unroll
-        for (int cb = 0; cb < DH / 32; ++cb) dq[cb] = mfma(reader.column(kt, hf, tt, cb), sf, dq[cb]);
+      for (int u = 0; u < 2 * kCB; ++u) {
+        const int w = u + 2 * kAhead - 1;
+        if (w < 2 * kCB) kc[w % (2 * kAhead)] = reader.column(kt, hf, w / kCB, w % kCB);
+        dq[u % kCB] = mfma(kc[u % (2 * kAhead)], sf[u / kCB], dq[u % kCB]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
   if (row_ok) store_row<DH>(static_cast<uint16_t*>(p.dQ), off, g, dq, p.scale);
 }
 
-template <int DH, bool SHARED>
+template <int DH, int PARTS, bool SHARED>
 int launch_kv(const GradParams& p) {
-  constexpr int kLds = 2 * (2 * TileDims<DH>::kBytes + kTile * 8) + (SHARED ? 6 * kWave * 4 : 0);
+  constexpr int kStages = 2 * (2 * TileDims<DH>::kBytes + kTile * 8) + (SHARED ? 6 * kWave * 4 : 0);
+  constexpr int kMeet = kKeys * DH * 4 * 2;
+  constexpr int kLds = PARTS == 2 && kMeet > kStages ? kMeet : kStages;
   const int64_t nug_rows = p.shared ? p.Kt : p.max_k, loc_rows = p.shared ? p.Sm : p.max_local;
   const int64_t nug = (nug_rows + kKeys - 1) / kKeys, loc = (loc_rows + kKeys - 1) / kKeys;
   const int64_t owners = (static_cast<int64_t>(p.H_kv) * (p.shared ? 1 : p.B) + 7) / 8 * 8;
   if ((nug + loc) * owners > 0x7fffffffLL) return DODO_ERR_UNSUPPORTED;
   if (nug + loc == 0) return DODO_OK;
-  const auto kern = grad_kv_kernel<DH, SHARED>;
+  if constexpr (PARTS == 1) {
+    // Eight wavefronts per 128 keys where the workgroups leave compute units idle and walk over many tiles (the sums' meeting costs
+    // some 5 us).  Four / eight, rows, heads over K/V heads, nuggets, local rows: 1 x 512, 64 over 8, 410, 640 128 / 99 us; 4 x 512
+    // 192 / 153; 1 x 1000, 32 over 8, 1000, 1000 134 / 103; 1 x 2048, 8 over 8, 410, 2048 71 / 59; 5 x 500, 64 over 8, 300, 533 195 /
+    // 200; 1 x 512, 32 over 32, 410, 640 37.5 / 40.8; 8 x 512 160 / 229.
+    const int64_t walked = static_cast<int64_t>(p.H / p.H_kv) * ((p.max_q + kTile - 1) / kTile);
+    if ((nug + loc) * owners < 2 * compute_units() && walked >= 16) return launch_kv<DH, 2, SHARED>(p);
+  }
+  const auto kern = grad_kv_kernel<DH, PARTS, SHARED>;
   const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kern), kLds);
   if (rc != DODO_OK) return rc;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((nug + loc) * owners)), dim3(kGradThreads), kLds, p.stream, p, static_cast<int>(nug),
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((nug + loc) * owners)), dim3(PARTS * kGradThreads), kLds, p.stream, p, static_cast<int>(nug),
                      static_cast<int>(loc));
   return launch_status();
 }
@@ -481,7 +545,7 @@ template <int DH>
 int launch_both(const GradParams& p) {
   const int rc = launch_q<DH>(p);  // (first: it makes the rows' statistics)
   if (rc != DODO_OK) return rc;
-  return p.shared ? launch_kv<DH, true>(p) : launch_kv<DH, false>(p);
+  return p.shared ? launch_kv<DH, 1, true>(p) : launch_kv<DH, 1, false>(p);
 }
 
 }  // namespace
