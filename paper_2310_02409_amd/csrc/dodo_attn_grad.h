@@ -28,13 +28,17 @@ struct Entry {
   int q0, q_b, k0, k_b, l0, m_b;
 };
 __device__ __forceinline__ Entry entry_of(const GradParams& p, int e) {
-  Entry s;
+  const int32_t *k_end_p = p.nug_len != nullptr ? p.nug_len + e : p.cu_nuggets + e + 1, *l_end_p = p.loc_len != nullptr ? p.loc_len + e : p.cu_local + e + 1;
+  Entry s;  // (six loads at once)
   s.q0 = p.cu_q[e];
-  s.q_b = p.cu_q[e + 1] - s.q0;
+  const int q_end = p.cu_q[e + 1];
   s.k0 = p.cu_nuggets[e];
-  s.k_b = p.nug_len != nullptr ? p.nug_len[e] : p.cu_nuggets[e + 1] - s.k0;
+  const int k_end = *k_end_p;
   s.l0 = p.cu_local[e];
-  s.m_b = p.loc_len != nullptr ? p.loc_len[e] : p.cu_local[e + 1] - s.l0;
+  const int l_end = *l_end_p;
+  s.q_b = q_end - s.q0;
+  s.k_b = p.nug_len != nullptr ? k_end : k_end - s.k0;
+  s.m_b = p.loc_len != nullptr ? l_end : l_end - s.l0;
   return s;
 }
 

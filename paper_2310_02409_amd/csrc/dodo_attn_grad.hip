@@ -252,6 +252,7 @@ int grad_entry(GradParams& p, int32_t d_h, int dtype, int layout, void* ws, size
   if (!aligned16(p.Q) || !aligned16(p.Kn) || !aligned16(p.Vn) || !aligned16(p.Kl) || !aligned16(p.Vl) || !aligned16(p.dO) || !aligned16(p.O) ||
       !aligned16(p.dQ) || !aligned16(p.dKn) || !aligned16(p.dVn) || !aligned16(p.dKl) || !aligned16(p.dVl) || !aligned16(ws))
     return DODO_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(p.H) * d_h >= 1 << 24) return DODO_ERR_UNSUPPORTED;  // (offsets between 128 rows in 32 bits)
   if (p.Sq * p.H > 0x7fffffffLL || p.Kt > 0x7fffffffLL || p.Sm > 0x7fffffffLL) return DODO_ERR_UNSUPPORTED;
   if (!nuggets && !locals && p.max_q == 0) return DODO_OK;
   if (p.max_q > 0 && (!ws || ws_bytes < workspace_bytes(p.Sq, p.H))) return DODO_ERR_WORKSPACE_TOO_SMALL;

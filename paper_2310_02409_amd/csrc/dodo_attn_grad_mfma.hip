@@ -115,15 +115,26 @@ __device__ __forceinline__ bf16x8 half_bf16(const floatx16& x, int t) {
   return __builtin_convertvector(h, bf16x8);
 }
 
-// Row `off` of a gradient from its transposed blocks: lane (row, g) holds channels 32 cb + 8 v4 + 4 g .. + 4.
+// 32 rows of a gradient from a wavefront's transposed blocks (lane (row, g) holds channels 32 cb + 8 v4 + 4 g .. + 4), through LDS, so
+// that a store instruction writes whole rows.  `lds` is the wavefront's own, kRowsOut bytes; row r < `rows` goes `stride` bytes after the one before.
 template <int DH>
-__device__ __forceinline__ void store_row(uint16_t* base, int64_t off, int g, const floatx16 (&acc)[DH / 32], float scale) {
+constexpr int kRowsOut = 32 * (DH * 2 + 16);
+template <int DH>
+__device__ __forceinline__ void store_rows(char* lds, uint16_t* to, uint32_t stride, int rows, const floatx16 (&acc)[DH / 32], float scale) {
+  constexpr int kRow = DH * 2 + 16, kPieces = DH / 8, kRows = kWave / kPieces;  // (16 bytes between rows spread them over the banks)
+  const int lane = lane_id();
 #pragma unroll
   for (int cb = 0; cb < DH / 32; ++cb)
 #pragma unroll
     for (int v4 = 0; v4 < 4; ++v4)
-      store4<DODO_DTYPE_BF16>(base, off + 32 * cb + 8 * v4 + 4 * g, acc[cb][4 * v4] * scale, acc[cb][4 * v4 + 1] * scale,
+      store4<DODO_DTYPE_BF16>(lds + (lane & 31) * kRow, 32 * cb + 8 * v4 + 4 * (lane >> 5), acc[cb][4 * v4] * scale, acc[cb][4 * v4 + 1] * scale,
                               acc[cb][4 * v4 + 2] * scale, acc[cb][4 * v4 + 3] * scale);
+#pragma unroll
+  for (int u = 0; u < 32 / kRows; ++u) {
+    const int r = u * kRows + lane / kPieces, piece = lane % kPieces;
+    const uint4 v = *reinterpret_cast<const uint4*>(lds + r * kRow + piece * 16);
+    if (r < rows) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(to) + static_cast<uint32_t>(r) * stride + piece * 16) = v;
+  }
 }
 
 // ---- dK, dV ------------------------------------------------------------------------------------------------------------
@@ -169,20 +180,24 @@ __global__ __launch_bounds__(PARTS * kGradThreads, PARTS == 1 ? 2 : 1) void grad
   reader.init(lane);
 
   // fragments of the owned keys: lane (n, g) holds channels 16 ks + 8 g .. + 8 of key n
-  auto key_offset = [&](int l) { return (t.first + min(blk * 32 + l, t.rows - 1)) * t.tok_stride + t.kvh * t.head_stride; };
-  const int64_t off = key_offset(n);
   bf16x8 kf[DH / 16], vf[DH / 16];
+  auto load_keys = [&]() {
+    const int64_t first = t.first * t.tok_stride + t.kvh * t.head_stride;
+    const char *K = reinterpret_cast<const char*>(static_cast<const uint16_t*>(t.K) + first), *V = reinterpret_cast<const char*>(static_cast<const uint16_t*>(t.V) + first);
+    const uint32_t off = static_cast<uint32_t>(min(blk * 32 + n, t.rows - 1)) * static_cast<uint32_t>(t.tok_stride * 2) + 16 * g;
 #pragma unroll
-  for (int ks = 0; ks < DH / 16; ++ks) {
-    kf[ks] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(t.K) + off + 16 * ks + 8 * g);
-    vf[ks] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(t.V) + off + 16 * ks + 8 * g);
-  }
+    for (int ks = 0; ks < DH / 16; ++ks) {
+      kf[ks] = *reinterpret_cast<const bf16x8*>(K + off + 32 * ks);
+      vf[ks] = *reinterpret_cast<const bf16x8*>(V + off + 32 * ks);
+    }
+    // (used here for the compiler's eyes, so that its waits for them stand before the loop)
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks) asm volatile("" : "+v"(kf[ks]), "+v"(vf[ks]));
+  };
+  if (SHARED) load_keys();
   floatx16 dk[DH / 32], dv[DH / 32];
 #pragma unroll
   for (int cb = 0; cb < DH / 32; ++cb) dk[cb] = dv[cb] = zero16();
-  // (the fragments are used here for the compiler's eyes, so that its waits for them stand before the loop)
-#pragma unroll
-  for (int ks = 0; ks < DH / 16; ++ks) asm volatile("" : "+v"(kf[ks]), "+v"(vf[ks]));
 
   int e0 = t.entry0;
   do {
@@ -247,6 +262,7 @@ __global__ __launch_bounds__(PARTS * kGradThreads, PARTS == 1 ? 2 : 1) void grad
     };
     RowTile cur = entry_tile();
     if (cur.valid) issue(cur, 0);
+    if (!SHARED) load_keys();  // (behind the first tile's requests)
     for (int stage = 0; cur.valid; stage ^= 1) {
       char* const base = lds + stage * kStage;
       __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wavefront's part of the tile has landed
@@ -356,11 +372,12 @@ __global__ __launch_bounds__(PARTS * kGradThreads, PARTS == 1 ? 2 : 1) void grad
       dv[c / 16][c % 16] += meet[(kRegs + c) * kWave];
     }
   }
-  int l = n;
-  asm volatile("" : "+v"(l));  // (made again here: held through the loop, the offset's registers would be missing there)
-  if (l >= my_rows) return;
-  store_row<DH>(static_cast<uint16_t*>(t.dK), key_offset(l), g, dk, p.scale);
-  store_row<DH>(static_cast<uint16_t*>(t.dV), key_offset(l), g, dv, 1.f);
+  if (PARTS == 1) __syncthreads();  // the stages have been read (two parts: a wavefront's sums are its own)
+  if (!active) return;
+  char* out = lds + blk * (PARTS == 2 ? 2 * DH / 32 * 16 * kWave * 4 : kRowsOut<DH>);
+  const int64_t to = my_first * t.tok_stride + t.kvh * t.head_stride;
+  store_rows<DH>(out, static_cast<uint16_t*>(t.local ? p.dKl : p.dKn) + to, static_cast<uint32_t>(t.tok_stride * 2), my_rows, dk, p.scale);
+  store_rows<DH>(out, static_cast<uint16_t*>(t.local ? p.dVl : p.dVn) + to, static_cast<uint32_t>(t.tok_stride * 2), my_rows, dv, 1.f);
 }
 
 // ---- dQ ----------------------------------------------------------------------------------------------------------------
@@ -498,8 +515,14 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
       }
     }
   }
-  if (row_ok) store_row<DH>(static_cast<uint16_t*>(p.dQ), off, g, dq, p.scale);
+  __syncthreads();  // the stages have been read
+  if (!active) return;
+  store_rows<DH>(lds + wave * kRowsOut<DH>, static_cast<uint16_t*>(p.dQ) + (static_cast<int64_t>(s.q0 + w_i0) * p.H + h) * DH,
+                 static_cast<uint32_t>(p.H) * TD::kRowBytes, min(32, s.q_b - w_i0), dq, p.scale);
 }
+
+static_assert(kGradWaves * kRowsOut<128> <= 2 * 2 * TileDims<128>::kBytes && kGradWaves * kRowsOut<64> <= 2 * 2 * TileDims<64>::kBytes,
+              "the stages have room for the rows on their way out");
 
 template <int DH, int PARTS, bool SHARED>
 int launch_kv(const GradParams& p) {
