@@ -12,8 +12,8 @@
 namespace dodo {
 namespace {
 
-constexpr int kTokens = 8;      // consecutive tokens per workgroup
-constexpr int kMaxThreads = 512;
+constexpr int kTokens = 2;      // consecutive tokens per workgroup
+constexpr int kMaxThreads = 256;
 
 template <int DTYPE>
 __device__ __forceinline__ uint4 add16(const uint4& a, const uint4& b) {
@@ -66,7 +66,7 @@ __device__ __forceinline__ void write_row(const uint4* __restrict__ src, int64_t
         v = make_uint4(pack_bf16(acc[0], acc[1 % kElems]), pack_bf16(acc[2 % kElems], acc[3 % kElems]),
                        pack_bf16(acc[4 % kElems], acc[5 % kElems]), pack_bf16(acc[6 % kElems], acc[7 % kElems]));
     }
-    store16_stream(to + c, v);
+    to[c] = v;
   }
 }
 
@@ -78,38 +78,50 @@ struct GradRows {
   int64_t Kt, token_vec, src_layer_vec, dst_layer_vec;
 };
 
-// Grid: (chunk of kTokens tokens, tensor; layer).
+// Grid: (chunk of kTokens tokens; layer), K and V.
 template <int DTYPE, bool HEAD_MAJOR>
 __global__ __launch_bounds__(kMaxThreads) void scatter_rows_kernel(GradRows a) {
-  const bool is_v = blockIdx.x & 1;
-  const uint4* src = (is_v ? a.dVn : a.dKn) + blockIdx.y * a.src_layer_vec;
-  uint4* dst = (is_v ? a.dV : a.dK) + blockIdx.y * a.dst_layer_vec;
-  int64_t tok = static_cast<int64_t>(blockIdx.x >> 1) * kTokens;
+  const uint4 *dKn = a.dKn + blockIdx.y * a.src_layer_vec, *dVn = a.dVn + blockIdx.y * a.src_layer_vec;
+  uint4 *dK = a.dK + blockIdx.y * a.dst_layer_vec, *dV = a.dV + blockIdx.y * a.dst_layer_vec;
+  int64_t tok = static_cast<int64_t>(blockIdx.x) * kTokens;
   const int64_t end = tok + kTokens;
+  const SequenceLookup sequences(a.cu_seqlens, a.cu_nuggets, a.B);
   while (tok < end) {
-    const int b = sequence_of(a.cu_seqlens, a.B, tok);
-    if (b < 0) return;  // behind the last sequence
-    const int s0 = a.cu_seqlens[b], s1 = a.cu_seqlens[b + 1];
-    const int p0 = a.cu_nuggets[b], k_b = a.cu_nuggets[b + 1] - p0;
+    int s0, s1, p0, p1;
+    if (!sequences.find(tok, s0, s1, p0, p1)) return;  // behind the last sequence
+    const int k_b = p1 - p0;
     const int32_t* list = a.nugget_idx + p0;
     const int stop = static_cast<int>(min(end, static_cast<int64_t>(s1)) - s0);
+    const auto write = [&](int token, int first, int cnt) {
+      const int64_t to = (s0 + static_cast<int64_t>(token)) * a.token_vec;
+      write_row<DTYPE, HEAD_MAJOR, false>(dKn, p0 + first, cnt, a.Kt, a.vec_per_head, a.vec_per_row, dK + to);
+      write_row<DTYPE, HEAD_MAJOR, false>(dVn, p0 + first, cnt, a.Kt, a.vec_per_head, a.vec_per_row, dV + to);
+    };
     int t = static_cast<int>(tok - s0);
-    int p = lower_bound_wave(list, k_b, t);
-    int seen = p, entry = 0;  // lane l holds list[seen + l]
-    bool loaded = false;
+    int seen = before_lower_bound(list, k_b, t);  // lane l holds list[seen + l]
+    int entry = seen + lane_id() < k_b ? list[seen + lane_id()] : 0x7fffffff;
+    if (~__ballot(entry < stop) != 0) {  // the 64 entries reach past these tokens (but for long runs of one index, always)
+      // the rows of zeros first: they wait for nothing
+      for (int z = t; z < stop; ++z)
+        if (__ballot(entry == z) == 0) write(z, 0, 0);
+      for (; t < stop; ++t) {
+        const uint64_t mine = __ballot(entry == t);
+        if (mine != 0) write(t, seen + __ffsll(static_cast<long long>(mine)) - 1, __popcll(mine));
+      }
+    }
+    int p = seen + __popcll(__ballot(entry < t));
     for (; t < stop; ++t) {
       const int first = p;
       while (true) {
-        if (!loaded || p >= seen + kWave) {
+        if (p >= seen + kWave) {
           seen = p;
           entry = seen + lane_id() < k_b ? list[seen + lane_id()] : 0x7fffffff;
-          loaded = true;
         }
         const int mine = __popcll(__ballot(entry == t && seen + lane_id() >= p));
         p += mine;
         if (p < seen + kWave) break;  // (a run of equal indices may go on in the next 64)
       }
-      write_row<DTYPE, HEAD_MAJOR, false>(src, p0 + first, p - first, a.Kt, a.vec_per_head, a.vec_per_row, dst + (s0 + static_cast<int64_t>(t)) * a.token_vec);
+      write(t, first, p - first);
     }
     tok = s0 + static_cast<int64_t>(stop);
   }
@@ -161,7 +173,7 @@ int gather_grad_entry(const void* dKn, const void* dVn, int dtype, const int32_t
   a.src_layer_vec = src_layer_stride * es / 16; a.dst_layer_vec = dst_layer_stride * es / 16;
   const int threads = min(kMaxThreads, (a.vec_per_row + kWave - 1) / kWave * kWave);
   const int64_t items = accumulate ? Kt : (N + kTokens - 1) / kTokens;
-  const dim3 grid(static_cast<unsigned>(2 * items), static_cast<unsigned>(L)), block(static_cast<unsigned>(threads));
+  const dim3 grid(static_cast<unsigned>(accumulate ? 2 * items : items), static_cast<unsigned>(L)), block(static_cast<unsigned>(threads));
   const bool hm = layout == DODO_LAYOUT_HEAD_MAJOR, f32 = dtype == DODO_DTYPE_F32;
   const auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, static_cast<hipStream_t>(stream), a); };
   if (accumulate) {

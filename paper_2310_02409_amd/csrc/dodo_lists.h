@@ -22,19 +22,52 @@ __device__ __forceinline__ int sequence_of(const int32_t* __restrict__ cu, int B
   return lo;
 }
 
-// First position p of list[0 .. n) (ascending) with list[p] >= value, n if there is none.  Called by whole wavefronts: 64 places
-// are looked at in each step, so a list of 4096 takes two memory latencies.
-__device__ __forceinline__ int lower_bound_wave(const int32_t* __restrict__ list, int n, int value) {
-  int lo = 0, hi = n;  // the answer is in [lo, hi]
-  while (hi > lo) {
-    const int step = (hi - lo + kWave - 1) / kWave;
-    const int at = lo + lane_id() * step;
-    const uint64_t below = __ballot(at < hi && list[min(at, hi - 1)] < value);  // a run of lanes from 0 on
-    const int cnt = __popcll(below);
+// The sequences' token and nugget ranges, found by token.  Up to 64 sequences: a sequence per lane, all of it fetched at once.
+struct SequenceLookup {
+  const int32_t *cu_seqlens, *cu_nuggets;
+  int B, s0_l, s1_l, k0_l, k1_l;
+  __device__ __forceinline__ SequenceLookup(const int32_t* cu_seqlens_, const int32_t* cu_nuggets_, int B_)
+      : cu_seqlens(cu_seqlens_), cu_nuggets(cu_nuggets_), B(B_) {
+    if (B <= kWave) {
+      const int lane = lane_id();
+      s0_l = cu_seqlens[min(lane, B)];
+      s1_l = cu_seqlens[min(lane + 1, B)];
+      k0_l = cu_nuggets[min(lane, B)];
+      k1_l = cu_nuggets[min(lane + 1, B)];
+    }
+  }
+  // Ranges [s0, s1) of tokens and [k0, k1) of nuggets of the sequence that token `tok` belongs to; false behind the last one.
+  __device__ __forceinline__ bool find(int64_t tok, int& s0, int& s1, int& k0, int& k1) const {
+    if (B <= kWave) {
+      const uint64_t above = __ballot(lane_id() < B && s1_l > tok);
+      if (above == 0) return false;
+      const int b = __ffsll(static_cast<long long>(above)) - 1;
+      s0 = __builtin_amdgcn_readlane(s0_l, b);
+      s1 = __builtin_amdgcn_readlane(s1_l, b);
+      k0 = __builtin_amdgcn_readlane(k0_l, b);
+      k1 = __builtin_amdgcn_readlane(k1_l, b);
+      return true;
+    }
+    const int b = sequence_of(cu_seqlens, B, tok);
+    if (b < 0) return false;
+    s0 = cu_seqlens[b];
+    s1 = cu_seqlens[b + 1];
+    k0 = cu_nuggets[b];
+    k1 = cu_nuggets[b + 1];
+    return true;
+  }
+};
+
+// A place p0 <= p in list[0 .. n) (ascending), where p is the first with list[p] >= value (n if there is none), no more than 64 before
+// it.  64 places are looked at in each step: one memory latency for a list of up to 4096.
+__device__ __forceinline__ int before_lower_bound(const int32_t* __restrict__ list, int n, int value) {
+  int lo = 0, hi = n;  // p is in [lo, hi]
+  while (hi - lo > kWave) {
+    const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane_id() * step;
+    const int cnt = __popcll(__ballot(at < hi && list[min(at, hi - 1)] < value));  // a run of lanes from 0 on
     if (cnt == 0) return lo;
-    const int last = lo + (cnt - 1) * step;  // the last place looked at that is below
-    hi = min(hi, last + step);
-    lo = last + 1;
+    lo += (cnt - 1) * step + 1;  // behind the last place looked at that is below
+    hi = min(hi, lo - 1 + step);
   }
   return lo;
 }
