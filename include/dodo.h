@@ -469,13 +469,16 @@ int dodo_unpack_nuggets_q4(const uint8_t* Kc, const uint8_t* Ks, const uint8_t* 
 
 /*
  * dodo_nugget_attention over a nugget cache in 4 bits (Kc, Ks, Vc, Vs in `layout`, Kt rows); the local rows, Q and O are of
- * `dtype`.  Same arguments, causal rule and result as dodo_nugget_attention over the unpacked cache: logits, sums and
- * the weights' products are fp32 sums of exact products of bf16 numbers, whose weights are rounded as there.  Supported:
- * d_h in {64, 128}, fp32 or bf16.
- * ws: dodo_nugget_attention_q4_workspace_bytes bytes, 16-byte aligned, zero-filled before its first use; a call leaves it so that
- * calls with the same arguments can use it again as it is (fill it with zeros before a call with other ones, and after a
- * call that was aborted).  It must not be shared by calls that may overlap in time.
+ * `dtype`.  Same arguments and causal rule as dodo_nugget_attention, and the result that it gives over the unpacked cache but for the
+ * rounding of intermediates: bf16 products are exact, sums fp32, weights rounded to bf16 (twice as many bits for few query rows).
+ * Few query rows (bf16, max_q < DODO_ATTENTION_BLOCK_MIN_Q, at most 32 query heads per K/V head) read the codes
+ * where they are; other calls unpack the cache into the workspace first.  Deterministic.  Supported: d_h in {64, 128}, fp32 or bf16.
+ * A block whose scale byte is 255 makes NaN of the heads' rows that see it (K) or of its 32 channels of them (V).
+ * ws: dodo_nugget_attention_q4_workspace_bytes bytes (may be 0), 16-byte aligned, the first DODO_Q4_ZEROED_BYTES of it (or all, where
+ * it is smaller) filled with zeros before its first use.  A call leaves these as zeros, so any later call that the size serves can
+ * use it as it is; after a call that was aborted they are filled again.  It must not be shared by calls that may overlap in time.
  */
+#define DODO_Q4_ZEROED_BYTES 65536
 size_t dodo_nugget_attention_q4_workspace_bytes(int32_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int32_t max_k,
                                                 int32_t max_local, int64_t Kt, int dtype);
 int dodo_nugget_attention_q4(const void* Q, const uint8_t* Kc, const uint8_t* Ks, const uint8_t* Vc, const uint8_t* Vs,

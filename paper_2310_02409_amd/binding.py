@@ -21,6 +21,7 @@ F32, BF16 = 0, 1
 RELU, GELU, TANH = 0, 1, 2
 FORCE_LAST = 1
 TOKEN_MAJOR, HEAD_MAJOR = 0, 1
+_Q4_ZEROED_BYTES = 65536  # DODO_Q4_ZEROED_BYTES
 
 
 class DodoError(RuntimeError):
@@ -840,7 +841,8 @@ def dodo_nugget_attention_q4(Q: torch.Tensor, Kc: torch.Tensor, Ks: torch.Tensor
     code = _dtype_code(Q)
     need = dodo_nugget_attention_q4_workspace_bytes(B, H, H_kv, d_h, max_q, max_k, max_local, Kt, code)
     if need and ws is None:
-        ws = torch.zeros(need, dtype=torch.uint8, device=Q.device)
+        ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
+        ws[:_Q4_ZEROED_BYTES].zero_()
     _check(lib.dodo_nugget_attention_q4(_ptr(Q), _ptr(Kc), _ptr(Ks), _ptr(Vc), _ptr(Vs), _ptr(Kl), _ptr(Vl), _ptr(cu_q), _ptr(cu_nuggets),
                                         _ptr(cu_local), B, H, H_kv, d_h, max_q, max_k, max_local, Kt, float(softmax_scale), code, layout,
                                         _ptr(O), _ptr(lse), *_workspace(ws), _stream()), "dodo_nugget_attention_q4")

@@ -168,7 +168,7 @@ def test_wide_scales_and_large_logits(D):
         check(D, t, lens, scale, BF16, O, lse)
 
 
-@pytest.mark.parametrize("q", [40])
+@pytest.mark.parametrize("q", [1, 5, 40])
 def test_a_bad_block_reaches_its_own_head_and_channels(D, q):
     lens, H, d_h = ([q, q], [70, 40], [q + 3, q]), 2, 128
     t = attention_case(22, *lens, H, H, d_h, BF16)
