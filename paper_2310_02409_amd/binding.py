@@ -21,7 +21,6 @@ F32, BF16 = 0, 1
 RELU, GELU, TANH = 0, 1, 2
 FORCE_LAST = 1
 TOKEN_MAJOR, HEAD_MAJOR = 0, 1
-_Q4_ZEROED_BYTES = 65536  # DODO_Q4_ZEROED_BYTES
 
 
 class DodoError(RuntimeError):
@@ -151,8 +150,12 @@ _native.bind(_raise_status, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
     lib.dodo_nugget_attention_workspace_bytes_grouped, lib.dodo_nugget_attention, lib.dodo_nugget_attention_indexed,
     lib.dodo_nugget_attention_cached, lib.dodo_stream_append, lib.dodo_score_mlp_workspace_bytes, lib.dodo_score_mlp,
     lib.dodo_threshold_from_sample_workspace_bytes, lib.dodo_threshold_from_sample, lib.dodo_select_threshold, lib.dodo_segment_plan,
-    lib.dodo_nugget_attention_segments, lib.dodo_ste_score_grad_workspace_bytes, lib.dodo_ste_score_grad)))
+    lib.dodo_nugget_attention_segments, lib.dodo_ste_score_grad_workspace_bytes, lib.dodo_ste_score_grad,
+    lib.dodo_nugget_attention_grad_workspace_bytes, lib.dodo_nugget_attention_grad, lib.dodo_nugget_attention_segments_grad,
+    lib.dodo_gather_nuggets_grad, lib.dodo_gather_nuggets_q4, lib.dodo_unpack_nuggets_q4, lib.dodo_nugget_attention_q4_workspace_bytes,
+    lib.dodo_nugget_attention_q4)))
 _BLOCK_MIN_Q = _native.ATTENTION_BLOCK_MIN_Q  # the header's
+_Q4_ZEROED_BYTES = _native.Q4_ZEROED_BYTES  # likewise
 _current_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
@@ -637,6 +640,10 @@ def dodo_nugget_attention_grad(Q: torch.Tensor, Kn: torch.Tensor, Vn: torch.Tens
                                dQ: Optional[torch.Tensor] = None, dKn: Optional[torch.Tensor] = None, dVn: Optional[torch.Tensor] = None,
                                dKl: Optional[torch.Tensor] = None, dVl: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """Gradients of dodo_nugget_attention from dO, with its O and lse; returns (dQ, dKn, dVn, dKl, dVl) in the inputs' shapes."""
+    done = _native.nugget_attention_grad(Q, Kn, Vn, Kl, Vl, dO, O, lse, cu_q, cu_nuggets, cu_local, max_q, max_k, max_local, softmax_scale,
+                                         layout, dQ, dKn, dVn, dKl, dVl, ws)
+    if done is not None:
+        return done
     if not cu_q.numel() == cu_nuggets.numel() == cu_local.numel():
         raise ValueError("cu_q, cu_nuggets and cu_local have to be of one length")
     return _attention_grad(lib.dodo_nugget_attention_grad, "dodo_nugget_attention_grad", Q, Kn, Vn, Kl, Vl, dO, O, lse,
@@ -653,6 +660,10 @@ def dodo_nugget_attention_segments_grad(Q: torch.Tensor, Kn: torch.Tensor, Vn: t
                                         dVn: Optional[torch.Tensor] = None, dK: Optional[torch.Tensor] = None,
                                         dV: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """Gradients of dodo_nugget_attention_segments, those of shared rows summed over the entries; returns (dQ, dKn, dVn, dK, dV)."""
+    done = _native.nugget_attention_segments_grad(Q, Kn, Vn, K, V, dO, O, lse, seg_cu_q, seg_nug_start, seg_nug_len, seg_loc_start, seg_loc_len,
+                                                  max_q, max_k, max_local, softmax_scale, layout, dQ, dKn, dVn, dK, dV, ws)
+    if done is not None:
+        return done
     n_seg = seg_cu_q.numel() - 1
     for t in (seg_nug_start, seg_nug_len, seg_loc_start, seg_loc_len):
         if t.numel() != n_seg:
@@ -667,6 +678,9 @@ def dodo_gather_nuggets_grad(dKn: torch.Tensor, dVn: torch.Tensor, nugget_idx: t
                              dV: Optional[torch.Tensor] = None, accumulate: bool = False):
     """Gradient of dodo_gather_nuggets: the cache's gradient rows back at their tokens, zeros elsewhere; with accumulate they are
     added to dK, dV instead.  Returns (dK, dV) [N, H_kv, d_h]."""
+    done = _native.gather_nuggets_grad(dKn, dVn, nugget_idx, cu_seqlens, cu_nuggets, total_tokens, layout, dK, dV, accumulate)
+    if done is not None:
+        return done
     _same_device(dKn, dVn, nugget_idx, cu_seqlens, cu_nuggets, dK, dV)
     _dev(dKn, dVn, nugget_idx, cu_seqlens, cu_nuggets)
     _int32(nugget_idx, cu_seqlens, cu_nuggets)
@@ -747,6 +761,9 @@ def dodo_gather_nuggets_q4(K: torch.Tensor, V: torch.Tensor, nugget_idx: torch.T
                            total_nuggets: int, layout: int = TOKEN_MAJOR, Kc: Optional[torch.Tensor] = None,
                            Ks: Optional[torch.Tensor] = None, Vc: Optional[torch.Tensor] = None, Vs: Optional[torch.Tensor] = None):
     """Packs the chosen rows of K, V [N, H_kv, d_h] into a nugget cache in 4 bits; returns codes and scales (Kc, Ks, Vc, Vs)."""
+    done = _native.gather_nuggets_q4(K, V, nugget_idx, cu_seqlens, cu_nuggets, total_nuggets, layout, Kc, Ks, Vc, Vs)
+    if done is not None:
+        return done
     _same_device(K, V, nugget_idx, cu_seqlens, cu_nuggets, Kc, Ks, Vc, Vs)
     _dev(nugget_idx, cu_seqlens, cu_nuggets, Kc, Ks, Vc, Vs)
     _dev_rows(K, V)
@@ -787,6 +804,9 @@ def dodo_gather_nuggets_q4_layers(K: torch.Tensor, V: torch.Tensor, nugget_idx: 
 def dodo_unpack_nuggets_q4(Kc: torch.Tensor, Ks: torch.Tensor, Vc: torch.Tensor, Vs: torch.Tensor, dtype: torch.dtype = torch.bfloat16,
                            Kn: Optional[torch.Tensor] = None, Vn: Optional[torch.Tensor] = None):
     """The plain nugget cache (of `dtype`) that a 4-bit one stands for, in its layout (any leading dimensions); returns (Kn, Vn)."""
+    done = _native.unpack_nuggets_q4(Kc, Ks, Vc, Vs, F32 if dtype is torch.float32 else BF16 if dtype is torch.bfloat16 else -1, Kn, Vn)
+    if done is not None:
+        return done
     _same_device(Kc, Ks, Vc, Vs, Kn, Vn)
     _dev(Kc, Ks, Vc, Vs, Kn, Vn)
     d_h = 2 * Kc.shape[-1]
@@ -817,6 +837,10 @@ def dodo_nugget_attention_q4(Q: torch.Tensor, Kc: torch.Tensor, Ks: torch.Tensor
                              O: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
                              ws: Optional[torch.Tensor] = None):
     """dodo_nugget_attention over a nugget cache in 4 bits (codes and scales of K and V); returns (O, lse or None)."""
+    done = _native.nugget_attention_q4(Q, Kc, Ks, Vc, Vs, Kl, Vl, cu_q, cu_nuggets, cu_local, max_q, max_k, max_local, softmax_scale, layout, O,
+                                       lse, want_lse, ws)
+    if done is not None:
+        return done
     _same_device(Q, Kc, Ks, Vc, Vs, Kl, Vl, cu_q, cu_nuggets, cu_local, O, lse, ws)
     _dev(Q, Kc, Ks, Vc, Vs, Kl, Vl, cu_q, cu_nuggets, cu_local, O, lse, ws)
     _int32(cu_q, cu_nuggets, cu_local)

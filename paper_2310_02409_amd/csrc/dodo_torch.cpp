@@ -15,6 +15,7 @@
 #include <cmath>
 #include <initializer_list>
 #include <limits>
+#include <utility>
 
 #include "dodo.h"
 
@@ -40,6 +41,14 @@ struct Entries {
   decltype(&dodo_nugget_attention_segments) attention_segments = nullptr;
   decltype(&dodo_ste_score_grad_workspace_bytes) ste_ws = nullptr;
   decltype(&dodo_ste_score_grad) ste = nullptr;
+  decltype(&dodo_nugget_attention_grad_workspace_bytes) attention_grad_ws = nullptr;
+  decltype(&dodo_nugget_attention_grad) attention_grad = nullptr;
+  decltype(&dodo_nugget_attention_segments_grad) attention_segments_grad = nullptr;
+  decltype(&dodo_gather_nuggets_grad) gather_grad = nullptr;
+  decltype(&dodo_gather_nuggets_q4) gather_q4 = nullptr;
+  decltype(&dodo_unpack_nuggets_q4) unpack_q4 = nullptr;
+  decltype(&dodo_nugget_attention_q4_workspace_bytes) attention_q4_ws = nullptr;
+  decltype(&dodo_nugget_attention_q4) attention_q4 = nullptr;
 } L;
 PyObject* raise_error = nullptr;
 
@@ -495,7 +504,276 @@ PyObject* ste_score_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-constexpr int kEntries = 18;
+// ---- gradients, and caches in 4 bits ----
+
+// All on the current device, whose stream the call goes to.
+void require_here(std::initializer_list<const at::Tensor*> tensors) {
+  const auto device = c10::hip::current_device();
+  for (const at::Tensor* t : tensors) require(!t->defined() || t->device().index() == device);
+}
+void require_shape(const at::Tensor& t, at::IntArrayRef shape, at::ScalarType type) { require(t.sizes() == shape && t.scalar_type() == type); }
+// The caller's result, in shape and type of `model`, or a new one.
+void like(at::Tensor& t, const at::Tensor& model) {
+  if (!t.defined()) t = at::empty_like(model);
+}
+// a tuple of results, an argument that is handed back being the caller's own object
+PyObject* tuple_of_results(std::initializer_list<std::pair<PyObject*, const at::Tensor*>> results) {
+  PyObject* all = PyTuple_New(static_cast<Py_ssize_t>(results.size()));
+  if (all == nullptr) return nullptr;
+  Py_ssize_t i = 0;
+  for (const auto& r : results) {
+    PyObject* o = same_or_new(r.first, *r.second);
+    if (o == nullptr) {
+      Py_DECREF(all);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(all, i++, o);
+  }
+  return all;
+}
+
+// The backward pass of nugget attention; `n_ranges` arrays of ranges behind the eight tensors.
+struct AttentionGradArgs {
+  const at::Tensor &Q, &Kn, &Vn, &Kl, &Vl, &dO, &O, &lse;
+  const at::Tensor* ranges[5] = {};
+  int32_t B, H, H_kv, d_h, max_q, max_k, max_local;
+  int64_t Sq, Kt, Sm;
+  int code, layout;
+  float scale;
+  at::Tensor dQ, dKn, dVn, dKl, dVl, ws;
+  PyObject* const* given;
+
+  AttentionGradArgs(PyObject* const* a, int n_ranges)
+      : Q(tensor(a[0])), Kn(tensor(a[1])), Vn(tensor(a[2])), Kl(tensor(a[3])), Vl(tensor(a[4])), dO(tensor(a[5])), O(tensor(a[6])), lse(tensor(a[7])) {
+    for (int i = 0; i < n_ranges; ++i) {
+      ranges[i] = &int32_tensor(a[8 + i]);
+      require(ranges[i]->dim() == 1);
+    }
+    PyObject* const* b = a + 8 + n_ranges;
+    max_q = int32(whole(b[0]));
+    max_k = int32(whole(b[1]));
+    max_local = int32(whole(b[2]));
+    require(Q.dim() == 3 && Kl.dim() == 3 && Kn.dim() == 3 && Q.size(2) > 0 && ranges[0]->numel() >= 1);
+    Sq = Q.size(0);
+    H = int32(Q.size(1));
+    d_h = int32(Q.size(2));
+    Sm = Kl.size(0);
+    H_kv = int32(Kl.size(1));
+    B = int32(ranges[0]->numel() - 1);
+    for (int i = 1; i < n_ranges; ++i) require(ranges[i]->numel() == (n_ranges == 3 ? B + 1 : B));
+    scale = static_cast<float>(b[3] == Py_None ? 1.0 / std::sqrt(static_cast<double>(d_h)) : real(b[3]));
+    layout = int32(whole(b[4]));
+    require(layout == DODO_LAYOUT_TOKEN_MAJOR || layout == DODO_LAYOUT_HEAD_MAJOR);
+    Kt = Kn.size(layout == DODO_LAYOUT_TOKEN_MAJOR ? 0 : 1);
+    code = dtype_code(Q);
+    const at::ScalarType type = Q.scalar_type();
+    const int64_t cache[3] = {layout == DODO_LAYOUT_TOKEN_MAJOR ? Kt : H_kv, layout == DODO_LAYOUT_TOKEN_MAJOR ? H_kv : Kt, d_h}, rows[2] = {Sq, H};
+    for (const at::Tensor* t : {&dO, &O}) require_shape(*t, Q.sizes(), type);
+    require_shape(lse, rows, at::kFloat);
+    for (const at::Tensor* t : {&Kn, &Vn}) require_shape(*t, cache, type);
+    require(Kl.size(2) == d_h);
+    for (const at::Tensor* t : {&Kl, &Vl}) require_shape(*t, Kl.sizes(), type);
+    given = b + 5;
+    at::Tensor* const outs[5] = {&dQ, &dKn, &dVn, &dKl, &dVl};
+    const at::Tensor* const models[5] = {&Q, &Kn, &Vn, &Kl, &Vl};
+    for (int i = 0; i < 5; ++i) {
+      *outs[i] = optional_tensor(given[i]);
+      if (outs[i]->defined()) require_shape(*outs[i], models[i]->sizes(), type);
+    }
+    ws = optional_tensor(given[5]);
+    require(!ws.defined() || ws.scalar_type() == at::kByte);
+    require_here({&Q, &Kn, &Vn, &Kl, &Vl, &dO, &O, &lse, &dQ, &dKn, &dVn, &dKl, &dVl, &ws});
+    for (int i = 0; i < n_ranges; ++i) require_here({ranges[i]});
+  }
+  void allocate() {
+    like(dQ, Q);
+    like(dKn, Kn);
+    like(dVn, Vn);
+    like(dKl, Kl);
+    like(dVl, Vl);
+    if (ws.defined()) return;
+    const size_t need = L.attention_grad_ws(B, H, H_kv, d_h, max_q, max_k, max_local, Sq, Kt, Sm, code);
+    if (need > 0) ws = at::empty({static_cast<int64_t>(need)}, Q.options().dtype(at::kByte));
+  }
+  PyObject* result() const { return tuple_of_results({{given[0], &dQ}, {given[1], &dKn}, {given[2], &dVn}, {given[3], &dKl}, {given[4], &dVl}}); }
+};
+
+PyObject* nugget_attention_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 22, [](PyObject* const* a) -> PyObject* {
+    AttentionGradArgs p(a, 3);
+    if (!run("dodo_nugget_attention_grad", [&] {
+          p.allocate();
+          return L.attention_grad(ptr(p.Q), ptr(p.Kn), ptr(p.Vn), ptr(p.Kl), ptr(p.Vl), ptr(p.dO), ptr(p.O), fptr(p.lse), iptr(*p.ranges[0]),
+                                  iptr(*p.ranges[1]), iptr(*p.ranges[2]), p.B, p.H, p.H_kv, p.d_h, p.max_q, p.max_k, p.max_local, p.Sq, p.Kt,
+                                  p.Sm, p.scale, p.code, p.layout, ptr(p.dQ), ptr(p.dKn), ptr(p.dVn), ptr(p.dKl), ptr(p.dVl), ptr(p.ws),
+                                  bytes_of(p.ws), stream());
+        }))
+      return nullptr;
+    return p.result();
+  });
+}
+
+PyObject* nugget_attention_segments_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 24, [](PyObject* const* a) -> PyObject* {
+    AttentionGradArgs p(a, 5);
+    if (!run("dodo_nugget_attention_segments_grad", [&] {
+          p.allocate();
+          return L.attention_segments_grad(ptr(p.Q), ptr(p.Kn), ptr(p.Vn), ptr(p.Kl), ptr(p.Vl), ptr(p.dO), ptr(p.O), fptr(p.lse),
+                                           iptr(*p.ranges[0]), iptr(*p.ranges[1]), iptr(*p.ranges[2]), iptr(*p.ranges[3]), iptr(*p.ranges[4]),
+                                           p.B, p.H, p.H_kv, p.d_h, p.max_q, p.max_k, p.max_local, p.Sq, p.Kt, p.Sm, p.scale, p.code, p.layout,
+                                           ptr(p.dQ), ptr(p.dKn), ptr(p.dVn), ptr(p.dKl), ptr(p.dVl), ptr(p.ws), bytes_of(p.ws), stream());
+        }))
+      return nullptr;
+    return p.result();
+  });
+}
+
+// What the gathers share: index list and the sequences' ranges.
+struct Lists {
+  const at::Tensor &idx, &cu_seqlens, &cu_nuggets;
+  int32_t B;
+  Lists(PyObject* i, PyObject* s, PyObject* k, int64_t total) : idx(int32_tensor(i)), cu_seqlens(int32_tensor(s)), cu_nuggets(int32_tensor(k)) {
+    require(idx.dim() == 1 && cu_seqlens.dim() == 1 && cu_nuggets.dim() == 1);
+    require(cu_seqlens.numel() >= 1 && cu_nuggets.numel() == cu_seqlens.numel() && total >= 0 && idx.numel() >= total);
+    B = int32(cu_seqlens.numel() - 1);
+    require_here({&idx, &cu_seqlens, &cu_nuggets});
+  }
+};
+
+PyObject* gather_nuggets_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 10, [](PyObject* const* a) -> PyObject* {
+    const at::Tensor &dKn = tensor(a[0]), &dVn = tensor(a[1]);
+    const int64_t N = whole(a[5]), layout = whole(a[6]);
+    at::Tensor dK = optional_tensor(a[7]), dV = optional_tensor(a[8]);
+    const bool accumulate = truth(a[9]), token = layout == DODO_LAYOUT_TOKEN_MAJOR;
+    require(dKn.dim() == 3 && N >= 0 && (token || layout == DODO_LAYOUT_HEAD_MAJOR) && dK.defined() == dV.defined() && (dK.defined() || !accumulate));
+    const int64_t Kt = dKn.size(token ? 0 : 1);
+    const int32_t h = int32(dKn.size(token ? 1 : 0)), dh = int32(dKn.size(2));
+    const Lists l(a[2], a[3], a[4], Kt);
+    const int code = dtype_code(dKn);
+    const int64_t shape[3] = {N, h, dh};
+    require_shape(dVn, dKn.sizes(), dKn.scalar_type());
+    if (dK.defined()) {
+      require_shape(dK, shape, dKn.scalar_type());
+      require_shape(dV, shape, dKn.scalar_type());
+    }
+    require_here({&dKn, &dVn, &dK, &dV});
+    if (!run("dodo_gather_nuggets_grad", [&] {
+          if (!dK.defined()) {
+            dK = at::empty(shape, dKn.options());
+            dV = at::empty(shape, dKn.options());
+          }
+          return L.gather_grad(ptr(dKn), ptr(dVn), code, iptr(l.idx), iptr(l.cu_seqlens), iptr(l.cu_nuggets), l.B, Kt, N, h, dh,
+                               static_cast<int64_t>(h) * dh, accumulate ? 1 : 0, ptr(dK), ptr(dV), static_cast<int>(layout), stream());
+        }))
+      return nullptr;
+    return tuple_of_results({{a[7], &dK}, {a[8], &dV}});
+  });
+}
+
+PyObject* gather_nuggets_q4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 11, [](PyObject* const* a) -> PyObject* {
+    const at::Tensor &K = tensor(a[0]), &V = tensor(a[1]);
+    const int64_t total = whole(a[5]), layout = whole(a[6]);
+    at::Tensor out[4];  // Kc, Ks, Vc, Vs
+    for (int i = 0; i < 4; ++i) {
+      out[i] = optional_tensor(a[7 + i]);
+      require(out[i].defined() == out[0].defined());
+    }
+    const bool token = layout == DODO_LAYOUT_TOKEN_MAJOR;
+    require(K.dim() == 3 && (token || layout == DODO_LAYOUT_HEAD_MAJOR));
+    require_shape(V, K.sizes(), K.scalar_type());
+    const Lists l(a[2], a[3], a[4], total);
+    const int code = dtype_code(K);
+    const int32_t h = int32(K.size(1)), dh = int32(K.size(2));
+    const int64_t codes[3] = {token ? total : h, token ? h : total, dh / 2}, scales[3] = {codes[0], codes[1], dh / 32};
+    if (out[0].defined())
+      for (int i = 0; i < 4; ++i) require_shape(out[i], i % 2 ? at::IntArrayRef(scales) : at::IntArrayRef(codes), at::kByte);
+    require_here({&K, &V, &out[0], &out[1], &out[2], &out[3]});
+    if (!run("dodo_gather_nuggets_q4", [&] {
+          const auto bytes = K.options().dtype(at::kByte);
+          if (!out[0].defined())
+            for (int i = 0; i < 4; ++i) out[i] = at::empty(i % 2 ? at::IntArrayRef(scales) : at::IntArrayRef(codes), bytes);
+          const auto byte_ptr = [](const at::Tensor& t) { return static_cast<uint8_t*>(ptr(t)); };
+          return L.gather_q4(ptr(K), ptr(V), code, iptr(l.idx), iptr(l.cu_seqlens), iptr(l.cu_nuggets), l.B, total, h, dh, static_cast<int64_t>(h) * dh,
+                             byte_ptr(out[0]), byte_ptr(out[1]), byte_ptr(out[2]), byte_ptr(out[3]), static_cast<int>(layout), stream());
+        }))
+      return nullptr;
+    return tuple_of_results({{a[7], &out[0]}, {a[8], &out[1]}, {a[9], &out[2]}, {a[10], &out[3]}});
+  });
+}
+
+// (code: of the type to unpack to)
+PyObject* unpack_nuggets_q4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 7, [](PyObject* const* a) -> PyObject* {
+    const at::Tensor &Kc = tensor(a[0]), &Ks = tensor(a[1]), &Vc = tensor(a[2]), &Vs = tensor(a[3]);
+    const int64_t code = whole(a[4]);
+    at::Tensor Kn = optional_tensor(a[5]), Vn = optional_tensor(a[6]);
+    require((code == DODO_DTYPE_F32 || code == DODO_DTYPE_BF16) && Kc.dim() >= 1);
+    const at::ScalarType type = code == DODO_DTYPE_F32 ? at::kFloat : at::kBFloat16;
+    c10::SmallVector<int64_t, 5> plain(Kc.sizes().begin(), Kc.sizes().end()), scales(plain);
+    plain.back() *= 2;
+    scales.back() = plain.back() / 32;
+    require_shape(Kc, Kc.sizes(), at::kByte);
+    require_shape(Vc, Kc.sizes(), at::kByte);
+    require_shape(Ks, scales, at::kByte);
+    require_shape(Vs, scales, at::kByte);
+    for (const at::Tensor* t : {&Kn, &Vn})
+      if (t->defined()) require_shape(*t, plain, type);
+    require_here({&Kc, &Ks, &Vc, &Vs, &Kn, &Vn});
+    const int32_t dh = int32(plain.back());
+    require(dh > 0);
+    if (!run("dodo_unpack_nuggets_q4", [&] {
+          for (at::Tensor* t : {&Kn, &Vn})
+            if (!t->defined()) *t = at::empty(plain, Kc.options().dtype(type));
+          const auto byte_ptr = [](const at::Tensor& t) { return static_cast<const uint8_t*>(ptr(t)); };
+          return L.unpack_q4(byte_ptr(Kc), byte_ptr(Ks), byte_ptr(Vc), byte_ptr(Vs), 2 * Kc.numel() / dh, dh, static_cast<int>(code), ptr(Kn), ptr(Vn),
+                             stream());
+        }))
+      return nullptr;
+    return tuple_of_results({{a[5], &Kn}, {a[6], &Vn}});
+  });
+}
+
+PyObject* nugget_attention_q4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded(args, n, 19, [](PyObject* const* a) -> PyObject* {
+    const at::Tensor* cache[4];  // Kc, Ks, Vc, Vs
+    for (int i = 0; i < 4; ++i) cache[i] = &tensor(a[1 + i]);
+    const at::Tensor &Kl = tensor(a[5]), &Vl = tensor(a[6]), &cu_n = int32_tensor(a[8]), &cu_l = int32_tensor(a[9]);
+    const int64_t layout = whole(a[14]);
+    AttentionArgs p(a[0], a[7], a[10], a[11], a[12], a[13], a[15], a[16], a[17], a[18]);
+    const bool token = layout == DODO_LAYOUT_TOKEN_MAJOR;
+    require(Kl.dim() == 3 && cache[0]->dim() == 3 && (token || layout == DODO_LAYOUT_HEAD_MAJOR));
+    const int32_t H_kv = int32(Kl.size(1));
+    const int64_t Kt = cache[0]->size(token ? 0 : 1);
+    const int64_t codes[3] = {token ? Kt : H_kv, token ? H_kv : Kt, p.d_h / 2}, scales[3] = {codes[0], codes[1], p.d_h / 32}, rows[2] = {p.Q.size(0), p.H};
+    for (int i = 0; i < 4; ++i) require_shape(*cache[i], i % 2 ? at::IntArrayRef(scales) : at::IntArrayRef(codes), at::kByte);
+    require(Kl.size(2) == p.d_h);
+    for (const at::Tensor* t : {&Kl, &Vl}) require_shape(*t, Kl.sizes(), p.Q.scalar_type());
+    if (p.O.defined()) require_shape(p.O, p.Q.sizes(), p.Q.scalar_type());
+    if (p.lse.defined()) require_shape(p.lse, rows, at::kFloat);
+    require(!p.ws.defined() || p.ws.scalar_type() == at::kByte);
+    require(p.cu_q.scalar_type() == at::kInt && cu_n.numel() == p.cu_q.numel() && cu_l.numel() == p.cu_q.numel());
+    require_here({&p.Q, cache[0], cache[1], cache[2], cache[3], &Kl, &Vl, &p.cu_q, &cu_n, &cu_l, &p.O, &p.lse, &p.ws});
+    if (!run("dodo_nugget_attention_q4", [&] {
+          like(p.O, p.Q);
+          if (!p.lse.defined() && p.want) p.lse = at::empty(rows, p.Q.options().dtype(at::kFloat));
+          const size_t need = p.ws.defined() ? 0 : L.attention_q4_ws(p.B, p.H, H_kv, p.d_h, p.max_q, p.max_k, p.max_local, Kt, p.code);
+          if (need > 0) {
+            p.ws = at::empty({static_cast<int64_t>(need)}, p.Q.options().dtype(at::kByte));
+            p.ws.narrow(0, 0, std::min<int64_t>(static_cast<int64_t>(need), DODO_Q4_ZEROED_BYTES)).zero_();
+          }
+          const auto byte_ptr = [](const at::Tensor* t) { return static_cast<const uint8_t*>(ptr(*t)); };
+          return L.attention_q4(ptr(p.Q), byte_ptr(cache[0]), byte_ptr(cache[1]), byte_ptr(cache[2]), byte_ptr(cache[3]), ptr(Kl), ptr(Vl),
+                                iptr(p.cu_q), iptr(cu_n), iptr(cu_l), p.B, p.H, H_kv, p.d_h, p.max_q, p.max_k, p.max_local, Kt, p.scale, p.code,
+                                static_cast<int>(layout), ptr(p.O), fptr(p.lse), ptr(p.ws), bytes_of(p.ws), stream());
+        }))
+      return nullptr;
+    return p.result();
+  });
+}
+
+constexpr int kEntries = 26;
 
 // bind(raise, address, ...): the function that raises the binding's error and the entry points, in the order of Entries
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -529,6 +807,14 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   L.attention_segments = reinterpret_cast<decltype(L.attention_segments)>(p[15]);
   L.ste_ws = reinterpret_cast<decltype(L.ste_ws)>(p[16]);
   L.ste = reinterpret_cast<decltype(L.ste)>(p[17]);
+  L.attention_grad_ws = reinterpret_cast<decltype(L.attention_grad_ws)>(p[18]);
+  L.attention_grad = reinterpret_cast<decltype(L.attention_grad)>(p[19]);
+  L.attention_segments_grad = reinterpret_cast<decltype(L.attention_segments_grad)>(p[20]);
+  L.gather_grad = reinterpret_cast<decltype(L.gather_grad)>(p[21]);
+  L.gather_q4 = reinterpret_cast<decltype(L.gather_q4)>(p[22]);
+  L.unpack_q4 = reinterpret_cast<decltype(L.unpack_q4)>(p[23]);
+  L.attention_q4_ws = reinterpret_cast<decltype(L.attention_q4_ws)>(p[24]);
+  L.attention_q4 = reinterpret_cast<decltype(L.attention_q4)>(p[25]);
   Py_INCREF(a[0]);
   Py_XDECREF(raise_error);
   raise_error = a[0];
@@ -539,14 +825,17 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {DODO_METHOD(bind), DODO_METHOD(score), DODO_METHOD(select_topk), DODO_METHOD(gather_nuggets),
                          DODO_METHOD(nugget_attention), DODO_METHOD(nugget_attention_indexed), DODO_METHOD(nugget_attention_cached),
                          DODO_METHOD(nugget_attention_segments), DODO_METHOD(stream_append), DODO_METHOD(score_mlp), DODO_METHOD(threshold_from_sample),
-                         DODO_METHOD(select_threshold), DODO_METHOD(segment_plan), DODO_METHOD(ste_score_grad), {nullptr, nullptr, 0, nullptr}};
+                         DODO_METHOD(select_threshold), DODO_METHOD(segment_plan), DODO_METHOD(ste_score_grad), DODO_METHOD(nugget_attention_grad),
+                         DODO_METHOD(nugget_attention_segments_grad), DODO_METHOD(gather_nuggets_grad), DODO_METHOD(gather_nuggets_q4),
+                         DODO_METHOD(unpack_nuggets_q4), DODO_METHOD(nugget_attention_q4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dodo_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
 PyMODINIT_FUNC PyInit__dodo_torch() {
   PyObject* m = PyModule_Create(&module);
-  if (m != nullptr && PyModule_AddIntConstant(m, "ATTENTION_BLOCK_MIN_Q", DODO_ATTENTION_BLOCK_MIN_Q) != 0) {
+  if (m != nullptr && (PyModule_AddIntConstant(m, "ATTENTION_BLOCK_MIN_Q", DODO_ATTENTION_BLOCK_MIN_Q) != 0 ||
+                       PyModule_AddIntConstant(m, "Q4_ZEROED_BYTES", DODO_Q4_ZEROED_BYTES) != 0)) {
     Py_DECREF(m);
     return nullptr;
   }
