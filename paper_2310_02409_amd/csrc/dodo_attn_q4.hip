@@ -21,6 +21,12 @@
 #include "dodo_attn_group.h"
 #include "dodo_q4.h"
 
+#ifndef AHEAD
+#define AHEAD 1
+#endif
+#ifndef UNITS
+#define UNITS 64
+#endif
 namespace dodo {
 namespace {
 
@@ -59,7 +65,8 @@ struct Q4Args {
   const uint16_t *Q, *Kl, *Vl;
   const uint8_t *Kc, *Ks, *Vc, *Vs;
   const int32_t *cu_q, *cu_nuggets, *cu_local;
-  int H, H_kv, G, max_q, rows_per, n_groups, nsplit;
+  int B, H, H_kv, G, max_q, rows_per, n_groups, nsplit;
+  int heads_per_unit, n_units;           // K/V heads that go to one XCD together, and the units of so many heads
   FastDiv div_G;
   int nug_cost, loc_cost;                // of a tile, for the shares
   int64_t row_stride, head_stride;       // of the nugget cache, in rows and heads of DH / 2 bytes of codes
@@ -90,22 +97,20 @@ __device__ __forceinline__ Codes<N> load_codes(const uint8_t* p) {
   }
   return c;
 }
-// Eight channels under a scale byte; a block that holds a NaN reads as NaN.
-__device__ __forceinline__ uint4 values8(uint32_t codes, uint32_t byte) {
-  const uint4 v = unpack8_bf16(codes, scale_q4(byte));
-  const uint32_t nan = byte == kScaleBadQ4 ? 0x7fc07fc0u : 0u;  // (of a code's conversion only infinities come with this byte)
-  return make_uint4(v.x | nan, v.y | nan, v.z | nan, v.w | nan);
-}
-
 template <int DH, int NV>
-__global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
+__global__ __launch_bounds__(kThreadsQ4, DH * NV > 2048 ? 1 : 2) void attention_q4_kernel(Q4Args a) {
   using QD = Q4Dims<DH, NV>;
   using Acc = typename Mfma<NV>::Acc;
   constexpr int kRowBytes = QD::kRowBytes, kP = QD::kP, kRowShift = QD::kRowShift, kCB = QD::kCB, kSteps = QD::kSteps;
   constexpr int kInstr = QD::kInstr, kRowsPerInstr = QD::kRowsPerInstr, kTensorBytes = QD::kTensorBytes, kWaveLds = QD::kWaveLds;
   constexpr int kPartStride = QD::kPartStride, kPARTS = 2;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int kvh = blockIdx.x, b = blockIdx.y, split = blockIdx.z % a.nsplit, group = blockIdx.z / a.nsplit;
+  // Block i runs on XCD i % 8.  A unit is a share of the keys of some neighbouring K/V heads of a sequence: token by token their codes
+  // and scales lie in the same cache lines, which one XCD's L2 then fetches once.
+  const int slot = blockIdx.x >> 3, unit = slot / a.heads_per_unit * 8 + (blockIdx.x & 7);
+  if (unit >= a.n_units) return;
+  const int per_seq = a.H_kv / a.heads_per_unit, rest = unit / per_seq, z = rest / a.B;
+  const int kvh = unit % per_seq * a.heads_per_unit + slot % a.heads_per_unit, b = rest % a.B, split = z % a.nsplit, group = z / a.nsplit;
   const int q0 = a.cu_q[b], q_end = a.cu_q[b + 1], k0 = a.cu_nuggets[b], k_end = a.cu_nuggets[b + 1], l0 = a.cu_local[b], l_end = a.cu_local[b + 1];
   asm volatile("" ::"s"(q0), "s"(q_end), "s"(k0), "s"(k_end), "s"(l0), "s"(l_end));  // one round of loads
   const int q_b = min(q_end - q0, a.max_q), k_b = k_end - k0, m_b = l_end - l0, row0 = group * a.rows_per;
@@ -199,8 +204,11 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
     }
     return x;
   };
-  Tile next;
-  if (first < nug_end) next = load_tile(first);
+  constexpr int kTilesAhead = AHEAD;
+  Tile buf[kTilesAhead + 1];
+#pragma unroll
+  for (int c = 0; c < kTilesAhead; ++c)
+    if (first + c * kWavesQ4 < nug_end) buf[c] = load_tile(first + c * kWavesQ4);
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   __syncthreads();  // every wavefront's part of the query vectors has landed
   bf16x8 qf[kSteps];  // lane (j, g): channels kRun g + 8 ds .. + 8 of its vector
@@ -262,9 +270,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
   };
 
   // ---- nuggets ----
-  for (int t = first; t < nug_end; t += kWavesQ4) {
-    const Tile x = next;
-    if (t + kWavesQ4 < nug_end) next = load_tile(t + kWavesQ4);
+  auto nugget_tile = [&](int t, const Tile& x) {
     // V on its way to be turned around: 32 channels of a row per lane and pass
 #pragma unroll
     for (int c = 0; c < kVPasses; ++c) {
@@ -273,7 +279,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
       for (int i = 0; i < 4; ++i) {
         const int piece = 4 * v_blk + i, gran = piece / QD::kGranPieces;
         *reinterpret_cast<uint4*>(lds_w + kTensorBytes + r * kRowBytes +
-                                  (((gran ^ ((r >> kRowShift) & (kCB - 1))) * QD::kGranPieces + piece % QD::kGranPieces) << 4)) = values8(x.v[c].w[i], x.vs[c]);
+                                  (((gran ^ ((r >> kRowShift) & (kCB - 1))) * QD::kGranPieces + piece % QD::kGranPieces) << 4)) = unpack8_bf16(x.v[c].w[i], scale_q4(x.vs[c]));
       }
     }
     Acc acc_s[QD::kKeyBlocks];
@@ -282,11 +288,20 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
     for (int ds = 0; ds < kSteps; ++ds)
 #pragma unroll
       for (int kb = 0; kb < QD::kKeyBlocks; ++kb)
-        acc_s[kb] = Mfma<NV>::mul(__builtin_bit_cast(bf16x8, values8(x.k[kb].w[ds], x.ks[kb][8 * ds / kBlockQ4 % kKScales])), qf[ds], acc_s[kb]);
+        acc_s[kb] = Mfma<NV>::mul(__builtin_bit_cast(bf16x8, unpack8_bf16(x.k[kb].w[ds], scale_q4(x.ks[kb][8 * ds / kBlockQ4 % kKScales]))), qf[ds], acc_s[kb]);
     bf16x8 pf[kPARTS][kRegs / 8], vt[QD::kPvSteps][kCB];
     softmax(acc_s, k_b - t * kKeysQ4, pf);
     read_v(vt);
     add_v(vt, pf);
+  };
+  for (int t = first; t < nug_end; t += (kTilesAhead + 1) * kWavesQ4) {
+#pragma unroll
+    for (int c = 0; c <= kTilesAhead; ++c) {  // (every buffer has its registers: a copy would wait for the tile)
+      const int now = t + c * kWavesQ4, then = now + kTilesAhead * kWavesQ4;
+      if (now >= nug_end) break;
+      if (then < nug_end) buf[(c + kTilesAhead) % (kTilesAhead + 1)] = load_tile(then);
+      nugget_tile(now, buf[c]);
+    }
   }
   // ---- local rows ----
   if (l_first < l_end_tile) {
@@ -475,7 +490,8 @@ struct Plan {
 Plan plan_of(int32_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int32_t max_k, int32_t max_local, int dtype) {
   Plan p = {};
   const int64_t G = H / H_kv;
-  if (dtype != DODO_DTYPE_BF16 || G > kVectorsQ4 || max_q >= DODO_ATTENTION_BLOCK_MIN_Q || B > 65535) return p;
+  if (dtype != DODO_DTYPE_BF16 || G > kVectorsQ4 || max_q >= DODO_ATTENTION_BLOCK_MIN_Q) return p;
+  if (static_cast<int64_t>(B) * H_kv > 1 << 22) return p;  // (the grid, with up to 32 shares and 15 groups of rows)
   if (static_cast<int64_t>(H) * d_h >= 1 << 24) return p;  // (offsets between rows of a tile in 32 bits)
   p.direct = true;
   p.rows_per = static_cast<int>(kVectorsQ4 / G);
@@ -494,12 +510,11 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr size_t kCounterBytes = kCounters * sizeof(uint32_t);
 
 template <int DH, int NV>
-int launch_direct(const Q4Args& a, int32_t B, hipStream_t stream) {
+int launch_direct(const Q4Args& a, hipStream_t stream) {
   const auto kern = attention_q4_kernel<DH, NV>;
   const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kern), Q4Dims<DH, NV>::kLds);
   if (rc != DODO_OK) return rc;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(a.H_kv), static_cast<unsigned>(B), static_cast<unsigned>(a.nsplit * a.n_groups)),
-                     dim3(kThreadsQ4), (Q4Dims<DH, NV>::kLds), stream, a);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((a.n_units + 7) / 8 * 8 * a.heads_per_unit)), dim3(kThreadsQ4), (Q4Dims<DH, NV>::kLds), stream, a);
   return launch_status();
 }
 
@@ -544,7 +559,7 @@ extern "C" int dodo_nugget_attention_q4(const void* Q, const uint8_t* Kc, const 
     a.Q = static_cast<const uint16_t*>(Q); a.Kl = static_cast<const uint16_t*>(Kl); a.Vl = static_cast<const uint16_t*>(Vl);
     a.Kc = Kc; a.Ks = Ks; a.Vc = Vc; a.Vs = Vs;
     a.cu_q = cu_q; a.cu_nuggets = cu_nuggets; a.cu_local = cu_local;
-    a.H = H; a.H_kv = H_kv; a.G = H / H_kv; a.max_q = max_q; a.rows_per = plan.rows_per; a.n_groups = plan.n_groups; a.nsplit = plan.nsplit;
+    a.B = B; a.H = H; a.H_kv = H_kv; a.G = H / H_kv; a.max_q = max_q; a.rows_per = plan.rows_per; a.n_groups = plan.n_groups; a.nsplit = plan.nsplit;
     a.div_G = make_fast_div(static_cast<uint32_t>(a.G));
     a.nug_cost = kNugCost; a.loc_cost = kLocCost;
     a.row_stride = layout == DODO_LAYOUT_TOKEN_MAJOR ? H_kv : 1;
@@ -553,10 +568,15 @@ extern "C" int dodo_nugget_attention_q4(const void* Q, const uint8_t* Kc, const 
     a.O = static_cast<uint16_t*>(O); a.lse = lse;
     a.counters = static_cast<uint32_t*>(ws);
     a.records = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + kCounterBytes);
+    // As many heads to a unit as there are, but units for all of the eight XCDs alike.
+    a.heads_per_unit = layout == DODO_LAYOUT_TOKEN_MAJOR ? H_kv : 1;
+    const auto units = [&]() { return static_cast<int64_t>(B) * plan.nsplit * plan.n_groups * (H_kv / a.heads_per_unit); };
+    while (a.heads_per_unit % 2 == 0 && units() % 8 != 0 && units() < UNITS) a.heads_per_unit /= 2;
+    a.n_units = static_cast<int>(units());
     // the narrow tiles where their 16 columns hold a group's vectors
     const bool narrow = plan.rows_per * a.G <= 16;
-    if (d_h == 128) return narrow ? launch_direct<128, 16>(a, B, s) : launch_direct<128, 32>(a, B, s);
-    return narrow ? launch_direct<64, 16>(a, B, s) : launch_direct<64, 32>(a, B, s);
+    if (d_h == 128) return narrow ? launch_direct<128, 16>(a, s) : launch_direct<128, 32>(a, s);
+    return narrow ? launch_direct<64, 16>(a, s) : launch_direct<64, 32>(a, s);
   }
   const size_t attention = dodo_nugget_attention_workspace_bytes_grouped(B, H, H_kv, d_h, max_q, max_k, max_local, dtype);
   const size_t cache = round256(static_cast<size_t>(Kt) * H_kv * d_h * elem_bytes(dtype));

@@ -94,8 +94,7 @@ __global__ __launch_bounds__(256) void unpack_q4_kernel(const uint32_t* __restri
   if (u >= units) return;
   const uint32_t codes = (blockIdx.y ? Vc : Kc)[u];
   const uint32_t byte = (blockIdx.y ? Vs : Ks)[u >> 2];
-  uint4 v = unpack8_bf16(codes, scale_q4(byte));
-  if (byte == kScaleBadQ4) v = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+  const uint4 v = unpack8_bf16(codes, scale_q4(byte));
   void* out = blockIdx.y ? Vn : Kn;
   if (DTYPE == DODO_DTYPE_BF16) {
     store16_stream(static_cast<uint4*>(out) + u, v);
