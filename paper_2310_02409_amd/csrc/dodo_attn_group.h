@@ -67,7 +67,8 @@ __device__ __forceinline__ float vector_sum(float x) {
 // are whole, as in the split-K kernel: calls that come here only to be faster than there have these (with two, one value of O in 250
 // rounded to another neighbour than the 64-bit result does, with three one in 6000, as there; 6 sequences of 357 rows, 64 heads over 8
 // 6.6 -> 6.7 us, 14 of 457 9.2 -> 9.6).  No part of a weight is negative, nor zero unless the weight is: with an
-// infinity in V their products are that infinity.
+// infinity in V their products are that infinity.  A lower part is `least` at least, or the weight itself, which then counts twice: with
+// the default that shows where the keys of weight 1 have a V below 2^-100, which 4-bit blocks may hold and their kernel asks for less.
 // The exponent offset m_run of a vector is moved (and its sum and output accumulators rescaled) only when the tile's
 // maximum exceeds it by more than kSlack: the result does not depend on the offset, the weights stay below
 // 2^kSlack, and after the first tiles of a vector the output accumulators are hardly ever touched again (the rescale is
@@ -75,7 +76,8 @@ __device__ __forceinline__ float vector_sum(float x) {
 constexpr float kSlack = 8.f;
 template <bool MASK, int NV, int CB, int REGS, int PARTS>
 __device__ __forceinline__ void softmax_tile32(float (&acc)[REGS], int limit, int g, float scale_log2e, float& m_run,
-                                               float& l_run, typename Mfma<NV>::Acc (&acc_o)[CB], bf16x8 (&pf)[PARTS][REGS / 8]) {
+                                               float& l_run, typename Mfma<NV>::Acc (&acc_o)[CB], bf16x8 (&pf)[PARTS][REGS / 8],
+                                               float least = 1e-30f) {
   float tmax = kNegInf;
 #pragma unroll
   for (int v = 0; v < REGS; ++v) {
@@ -115,8 +117,8 @@ __device__ __forceinline__ void softmax_tile32(float (&acc)[REGS], int limit, in
       for (int part = 0; part < PARTS - 1; ++part) {
         const uint32_t b0 = __float_as_uint(r0), b1 = __float_as_uint(r1);
         high[part][v / 2] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);  // the upper halves: rounded towards zero
-        r0 = __builtin_amdgcn_fmed3f(r0 - __uint_as_float(b0 & 0xffff0000u), 1e-30f, p0);
-        r1 = __builtin_amdgcn_fmed3f(r1 - __uint_as_float(b1 & 0xffff0000u), 1e-30f, p1);
+        r0 = __builtin_amdgcn_fmed3f(r0 - __uint_as_float(b0 & 0xffff0000u), least, p0);
+        r1 = __builtin_amdgcn_fmed3f(r1 - __uint_as_float(b1 & 0xffff0000u), least, p1);
       }
       low[v] = r0;
       low[v + 1] = r1;

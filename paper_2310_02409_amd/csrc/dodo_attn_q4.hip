@@ -1,7 +1,7 @@
 // dodo_nugget_attention_q4: nugget attention (Eq. 13 / Eq. 9 of the Dodo paper) over a nugget cache held in 4 bits.
 //
 // Few query rows (bf16): one kernel reads the codes where they are, a quarter of a bf16 cache's bytes, and every one once for
-// up to 32 query vectors.  A workgroup owns a share of the keys of one (sequence, K/V head, group of query rows); each of its four
+// 16 or 32 query vectors.  A workgroup owns a share of the keys of one (sequence, K/V head, group of query rows); each of its four
 // wavefronts takes tiles of 32 keys of it, without a barrier in the loop:
 //   K      codes go straight to registers: the sum over channels may run in any order, so a lane takes consecutive channels of
 //          its key, whose codes are one load and whose scale is one byte (two bytes for 64 channels), and the query vectors'
@@ -21,12 +21,6 @@
 #include "dodo_attn_group.h"
 #include "dodo_q4.h"
 
-#ifndef AHEAD
-#define AHEAD 1
-#endif
-#ifndef UNITS
-#define UNITS 64
-#endif
 namespace dodo {
 namespace {
 
@@ -98,7 +92,7 @@ __device__ __forceinline__ Codes<N> load_codes(const uint8_t* p) {
   return c;
 }
 template <int DH, int NV>
-__global__ __launch_bounds__(kThreadsQ4, DH * NV > 2048 ? 1 : 2) void attention_q4_kernel(Q4Args a) {
+__global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
   using QD = Q4Dims<DH, NV>;
   using Acc = typename Mfma<NV>::Acc;
   constexpr int kRowBytes = QD::kRowBytes, kP = QD::kP, kRowShift = QD::kRowShift, kCB = QD::kCB, kSteps = QD::kSteps;
@@ -204,7 +198,9 @@ __global__ __launch_bounds__(kThreadsQ4, DH * NV > 2048 ? 1 : 2) void attention_
     }
     return x;
   };
-  constexpr int kTilesAhead = AHEAD;
+  // One tile ahead (2 and 3 are no faster); none where the wide tiles of 128 channels leave no registers for two workgroups on a compute
+  // unit with it (8 sequences, 32 rows of 32 heads, 410 nuggets 30.1 -> 22.0 us).
+  constexpr int kTilesAhead = DH * NV > 2048 ? 0 : 1;
   Tile buf[kTilesAhead + 1];
 #pragma unroll
   for (int c = 0; c < kTilesAhead; ++c)
@@ -234,9 +230,9 @@ __global__ __launch_bounds__(kThreadsQ4, DH * NV > 2048 ? 1 : 2) void attention_
 #pragma unroll
     for (int v = 0; v < kRegs; ++v) sv[v] = acc_s[v / Mfma<NV>::kRegs][v % Mfma<NV>::kRegs];
     if (__all(limit >= kKeysQ4)) {
-      softmax_tile32<false, NV>(sv, limit, g, a.scale_log2e, m_run, l_run, acc_o, pf);
+      softmax_tile32<false, NV>(sv, limit, g, a.scale_log2e, m_run, l_run, acc_o, pf, 0x1p-126f);
     } else {
-      softmax_tile32<true, NV>(sv, limit, g, a.scale_log2e, m_run, l_run, acc_o, pf);
+      softmax_tile32<true, NV>(sv, limit, g, a.scale_log2e, m_run, l_run, acc_o, pf, 0x1p-126f);
     }
   };
   auto read_v = [&](bf16x8 (&vt)[QD::kPvSteps][kCB]) {
@@ -483,24 +479,46 @@ constexpr int kNugCost = 1, kLocCost = 2;
 
 // How the direct kernel would take a call (bf16, d_h 64 or 128, at most kVectorsQ4 heads per K/V head).
 struct Plan {
-  bool direct;
+  bool direct, narrow;  // narrow: groups of up to 16 vectors
   int rows_per, n_groups, nsplit;
   size_t records;  // bytes behind the counters
 };
-Plan plan_of(int32_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int32_t max_k, int32_t max_local, int dtype) {
+Plan plan_of(int64_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int32_t max_k, int32_t max_local, int dtype) {
   Plan p = {};
   const int64_t G = H / H_kv;
-  if (dtype != DODO_DTYPE_BF16 || G > kVectorsQ4 || max_q >= DODO_ATTENTION_BLOCK_MIN_Q) return p;
+  // Up to 64 vectors a K/V head, and up to 15 rows whatever the heads; beyond, where the vectors read the cache several times, unpacking it
+  // once is the faster.  Here / unpacked, 8 sequences, 32 heads, 410 nuggets, 257 local rows: 16 rows 13.7 / 33.1 us, 32 rows 30.1 / 34.2, 64
+  // rows 34.9 / 35.4, 128 rows 63.2 / 40.7; 32 sequences, 32 rows 71.9 / 121; 64 heads over 8, 3277 nuggets, 16 rows 66.3 / 65.3, 64 rows 191 / 116.
+  if (dtype != DODO_DTYPE_BF16 || G > kVectorsQ4 || (max_q >= DODO_ATTENTION_BLOCK_MIN_Q && max_q * G > 2 * kVectorsQ4)) return p;
   if (static_cast<int64_t>(B) * H_kv > 1 << 22) return p;  // (the grid, with up to 32 shares and 15 groups of rows)
   if (static_cast<int64_t>(H) * d_h >= 1 << 24) return p;  // (offsets between rows of a tile in 32 bits)
   p.direct = true;
-  p.rows_per = static_cast<int>(kVectorsQ4 / G);
+  // Groups of 16 vectors where that leaves no compute unit with more than two workgroups, else of 32, which read the cache half as often.
+  // 16 / 32: 8 sequences, 32 heads, 410 nuggets, 257 local rows: 32 rows 17.3 / 22.0 us, 64 rows 30.6 / 22.6; 32 sequences, 32 rows 77.2 / 54.0;
+  // 64 heads over 8, 4 rows, 3277 nuggets, 1 sequence 14.9 / 19.7, 8 22.4 / 24.2.
+  const int64_t narrow_groups = (max_q * G + 15) / 16;
+  p.narrow = G <= 16 && (max_q * G <= 16 || static_cast<int64_t>(B) * H_kv * narrow_groups <= 2 * compute_units());
+  p.rows_per = static_cast<int>((p.narrow ? 16 : kVectorsQ4) / G);
   if (p.rows_per > max_q) p.rows_per = max_q;
   p.n_groups = (max_q + p.rows_per - 1) / p.rows_per;
-  const int64_t pairs = static_cast<int64_t>(B) * H_kv * p.n_groups, cus = compute_units();
-  const int64_t tiles = (static_cast<int64_t>(max_k) + kKeysQ4 - 1) / kKeysQ4 + (static_cast<int64_t>(max_local) + kKeysQ4 - 1) / kKeysQ4;
-  int64_t n = 1;
-  if (pairs <= kCounters) n = std::max<int64_t>(1, std::min<int64_t>({(2 * cus + pairs - 1) / pairs, tiles / kWavesQ4, kMaxSplitsQ4}));
+  const int64_t pairs = static_cast<int64_t>(B) * H_kv * p.n_groups, cus = compute_units(), vectors = p.rows_per * G;
+  const int64_t cost = (static_cast<int64_t>(max_k) + kKeysQ4 - 1) / kKeysQ4 * kNugCost + (static_cast<int64_t>(max_local) + kKeysQ4 - 1) / kKeysQ4 * kLocCost;
+  // The count of least expected time, in ns: a wavefront takes 900 for a tile of nuggets (twice that in the wide form) and as
+  // much again for a local one, half as much again where two workgroups share a compute unit; shares cost 2000, and the last workgroup
+  // reads 13 ns worth of records for each share and vector.  64 heads over 8, 3277 nuggets, 257 local rows: 1 sequence 13.5 / 11.4 / 10.9
+  // us in 28 / 14 / 16 shares, 2 of them with 1089 local rows 18.3 / 13.3 / 13.6 in 32 / 16 / 8, 8 15.4 / 16.6 in 8 / 4; 32 over 32, 410
+  // nuggets, 1 sequence 8.7 / 10.6 in 5 / 2, 8 with 4 rows 13.0 / 14.5 in 1 / 2, 16 22.9 / 28.3 in 1 / 2.
+  int64_t n = 1, best = 0;
+  for (int64_t s = 1; s <= kMaxSplitsQ4 && (s == 1 || (pairs <= kCounters && s * kWavesQ4 <= cost)); ++s) {
+    const int64_t workgroups = pairs * s;
+    const int64_t tile = (p.narrow ? 900 : 1800) * (workgroups <= cus ? 2 : 3) / 2;
+    const int64_t units = std::max<int64_t>((cost + s * kWavesQ4 - 1) / (s * kWavesQ4), max_local > 0 ? kLocCost : kNugCost);
+    const int64_t ns = std::max(units * tile, units * tile * workgroups / (2 * cus)) + (s == 1 ? 0 : 2000 + 13 * s * vectors);
+    if (s == 1 || ns < best) {
+      n = s;
+      best = ns;
+    }
+  }
   p.nsplit = static_cast<int>(n);
   p.records = n == 1 ? 0 : static_cast<size_t>(pairs) * p.rows_per * G * n * (d_h + 2) * sizeof(float);
   return p;
@@ -571,12 +589,10 @@ extern "C" int dodo_nugget_attention_q4(const void* Q, const uint8_t* Kc, const 
     // As many heads to a unit as there are, but units for all of the eight XCDs alike.
     a.heads_per_unit = layout == DODO_LAYOUT_TOKEN_MAJOR ? H_kv : 1;
     const auto units = [&]() { return static_cast<int64_t>(B) * plan.nsplit * plan.n_groups * (H_kv / a.heads_per_unit); };
-    while (a.heads_per_unit % 2 == 0 && units() % 8 != 0 && units() < UNITS) a.heads_per_unit /= 2;
+    while (a.heads_per_unit % 2 == 0 && units() % 8 != 0 && units() < 64) a.heads_per_unit /= 2;
     a.n_units = static_cast<int>(units());
-    // the narrow tiles where their 16 columns hold a group's vectors
-    const bool narrow = plan.rows_per * a.G <= 16;
-    if (d_h == 128) return narrow ? launch_direct<128, 16>(a, s) : launch_direct<128, 32>(a, s);
-    return narrow ? launch_direct<64, 16>(a, s) : launch_direct<64, 32>(a, s);
+    if (d_h == 128) return plan.narrow ? launch_direct<128, 16>(a, s) : launch_direct<128, 32>(a, s);
+    return plan.narrow ? launch_direct<64, 16>(a, s) : launch_direct<64, 32>(a, s);
   }
   const size_t attention = dodo_nugget_attention_workspace_bytes_grouped(B, H, H_kv, d_h, max_q, max_k, max_local, dtype);
   const size_t cache = round256(static_cast<size_t>(Kt) * H_kv * d_h * elem_bytes(dtype));
