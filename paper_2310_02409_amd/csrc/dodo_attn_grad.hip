@@ -12,221 +12,238 @@
 namespace dodo {
 namespace {
 
-typedef __attribute__((ext_vector_type(16))) float floatx16;
-
-// lse2[h][row] = lse[row,h] * log2(e) and neg_d[h][row] = -dO[row,h] . O[row,h], by heads, so that the rows of a head lie side by side.
-// A row that sees nothing (lse = -inf) gets +inf: its weights are 0.  16 lanes per (row, head).
-__global__ __launch_bounds__(256) void grad_rows_kernel(const float* __restrict__ dO, const float* __restrict__ O,
-                                                        const float* __restrict__ lse, int64_t Sq, int H, int d_h,
-                                                        float* __restrict__ lse2, float* __restrict__ neg_d) {
-  const int64_t t = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / 16;
-  if (t >= Sq * H) return;
-  const int sub = threadIdx.x % 16;
-  float acc = 0.f;
-  for (int c = sub * 4; c < d_h; c += 64) {
-    const float4 a = *reinterpret_cast<const float4*>(dO + t * d_h + c), o = *reinterpret_cast<const float4*>(O + t * d_h + c);
-    acc = fmaf(a.w, o.w, fmaf(a.z, o.z, fmaf(a.y, o.y, fmaf(a.x, o.x, acc))));
-  }
-  acc = lanes_sum<16>(acc);
-  if (sub == 0) {
-    const float l = lse[t];
-    lse2[(t % H) * Sq + t / H] = l == -__builtin_inff() ? __builtin_inff() : l * kLog2e;
-    neg_d[(t % H) * Sq + t / H] = -acc;
-  }
-}
-
 // ---- fp32 inputs, on the fp32 matrix instructions -------------------------------------------------------------------------
-// 32 x 32 blocks of S and dP from v_mfma_f32_32x32x2_f32; every wavefront fetches its fragments from memory itself.  A block's
-// accumulator v holds row 8 (v / 4) + 4 g + v % 4 (g = lane / 32) and the lane's column, which is just what the next product wants
-// as its right operand in step v, so P and dS stay where they are; the left operand's rows follow the same order.  The four
-// wavefronts of a workgroup take the walked tiles in turn and meet in LDS at the end, added in wavefront order.
+// 16 x 16 blocks of S and dP from v_mfma_f32_16x16x4_f32; every wavefront fetches its fragments from memory itself, 16 bytes a load.
+// Lane (n, g) = (lane % 16, lane / 16) owns row n of what the kernel sums.  A block's accumulator v holds walked row 4 g + v and the
+// lane's own one, which is just what the next product wants as its right operand in step v, so P and dS stay where they are; its
+// left operand, block 4 hi + e of the sums, takes channels 64 hi + 4 n + e, so that one load brings four blocks' and the sums are
+// stored four channels at a time.
+// A workgroup owns 16 rows; its wavefronts take the walked blocks in turn and their sums meet in LDS, added in wavefront order.  (64
+// rows, 16 a wavefront, walked together, is slower where it leaves compute units idle and little faster elsewhere.  This / that, dQ
+// and dK with dV, us: 1 sequence, 4 heads of 64, 32 rows, 51 nuggets, 48 local rows 6.7 + 6.7 / 10.5 + 9.2; 8 sequences, 32 heads of 128,
+// 512 rows, 410 nuggets, 640 local rows 1256 + 1422 / 1169 + 1379; 2, 2048 rows, 410, 2048 1871 + 2291 / 2490 + 2508; 8, 128 rows, 100, 256
+// 140 + 187 / 110 + 168.)  The large ones run at half of the fp32 matrix rate, 70 TFLOP/s; the smallest are a chain of loads: the
+// ranges, the owned rows, the walked rows, some 2 us each with the launch.
 
+constexpr int kPlainRows = 16;  // owned by a workgroup
 template <int DH>
-using OutBlocks = floatx16[DH / 32];
+using OutBlocks = floatx4[DH / 16];
 
 template <int DH>
 __device__ __forceinline__ void clear(OutBlocks<DH>& acc) {
 #pragma unroll
-  for (int cb = 0; cb < DH / 32; ++cb)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) acc[cb][v] = 0.f;
+  for (int cb = 0; cb < DH / 16; ++cb) acc[cb] = floatx4{0.f, 0.f, 0.f, 0.f};
 }
 
-// A row's channels as fragments: step 4 s + e of a product takes channel 8 s + 4 g + e.
+// A row's channels as fragments: step 4 s + e of a product takes channel 16 s + 4 g + e.
 template <int DH>
-__device__ __forceinline__ void load_row(const void* base, int64_t off, float (&f)[DH / 2]) {
+__device__ __forceinline__ void load_row(const void* base, int64_t off, float (&f)[DH / 4]) {
 #pragma unroll
-  for (int s = 0; s < DH / 8; ++s) {
+  for (int s = 0; s < DH / 16; ++s) {
     float x[4];
-    load4<DODO_DTYPE_F32>(base, off + 8 * s, x);
+    load4<DODO_DTYPE_F32>(base, off + 16 * s, x);
 #pragma unroll
     for (int e = 0; e < 4; ++e) f[4 * s + e] = x[e];
   }
 }
-// acc = (rows at base + off, one per lane) x (fragments of the columns)
+__device__ __forceinline__ floatx4 mfma(float a, float b, const floatx4& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+// s += (a's rows) x (k's columns), dp += (b's) x (v's)
 template <int DH>
-__device__ __forceinline__ floatx16 dot_rows(const void* base, int64_t off, const float (&f)[DH / 2]) {
-  floatx16 acc;
+__device__ __forceinline__ void dot_rows(const float (&a)[DH / 4], const float (&b)[DH / 4], const float (&k)[DH / 4], const float (&v)[DH / 4],
+                                         floatx4& s, floatx4& dp) {
 #pragma unroll
-  for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+  for (int c = 0; c < DH / 4; ++c) {
+    s = mfma(a[c], k[c], s);
+    dp = mfma(b[c], v[c], dp);
+  }
+}
+// acc += (walked row `base + off`, one per lane group g, as a column) x (w of the owned rows)
+template <int DH>
+__device__ __forceinline__ void add_column(OutBlocks<DH>& acc, const void* base, int64_t off, float w) {
 #pragma unroll
-  for (int s = 0; s < DH / 8; ++s) {
+  for (int hi = 0; hi < DH / 64; ++hi) {
     float x[4];
-    load4<DODO_DTYPE_F32>(base, off + 8 * s, x);
+    load4<DODO_DTYPE_F32>(base, off + 64 * hi, x);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], f[4 * s + e], acc, 0, 0, 0);
-  }
-  return acc;
-}
-
-// Sums of the workgroup's wavefronts, in wavefront order, in wavefront 0.
-template <int DH>
-__device__ __forceinline__ void sum_wavefronts(OutBlocks<DH>& acc, int wave, int lane, float* lds) {
-  for (int w = 1; w < kGradWaves; ++w) {
-    __syncthreads();
-    if (wave == w)
-#pragma unroll
-      for (int cb = 0; cb < DH / 32; ++cb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) lds[(cb * 16 + v) * kWave + lane] = acc[cb][v];
-    __syncthreads();
-    if (wave == 0)
-#pragma unroll
-      for (int cb = 0; cb < DH / 32; ++cb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[cb][v] += lds[(cb * 16 + v) * kWave + lane];
+    for (int e = 0; e < 4; ++e) acc[4 * hi + e] = mfma(x[e], w, acc[4 * hi + e]);
   }
 }
 
-// Row `off` of a gradient from the transposed blocks: lane (row, g) holds channels 32 cb + 8 v4 + 4 g .. + 4.
+// A row of a gradient: every wavefront puts its sums into LDS and then stores a quarter of all.
 template <int DH>
-__device__ __forceinline__ void store_row(void* base, int64_t off, int g, const OutBlocks<DH>& acc, float scale) {
+constexpr int kMeetWords = kGradWaves * DH / 16 * kWave;  // of 16 bytes, for one tensor
+template <int DH>
+__device__ __forceinline__ void put_sums(float4* lds, int wave, int lane, const OutBlocks<DH>& acc) {
 #pragma unroll
-  for (int cb = 0; cb < DH / 32; ++cb)
+  for (int hi = 0; hi < DH / 64; ++hi)
 #pragma unroll
-    for (int v4 = 0; v4 < 4; ++v4)
-      store4<DODO_DTYPE_F32>(base, off + 32 * cb + 8 * v4 + 4 * g, acc[cb][4 * v4] * scale, acc[cb][4 * v4 + 1] * scale,
-                    acc[cb][4 * v4 + 2] * scale, acc[cb][4 * v4 + 3] * scale);
+    for (int v = 0; v < 4; ++v)
+      lds[((wave * (DH / 64) + hi) * 4 + v) * kWave + lane] = make_float4(acc[4 * hi][v], acc[4 * hi + 1][v], acc[4 * hi + 2][v], acc[4 * hi + 3][v]);
+}
+template <int DH>
+__device__ __forceinline__ void store_sums(const float4* lds, int wave, int lane, void* base, int64_t off, bool row_ok, float scale) {
+#pragma unroll
+  for (int hi = 0; hi < DH / 64; ++hi) {
+    float4 sum = lds[(hi * 4 + wave) * kWave + lane];
+#pragma unroll
+    for (int w = 1; w < kGradWaves; ++w) {
+      const float4 x = lds[((w * (DH / 64) + hi) * 4 + wave) * kWave + lane];
+      sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+    }
+    if (row_ok) store4<DODO_DTYPE_F32>(base, off + 64 * hi + 16 * (lane >> 4) + 4 * wave, sum.x * scale, sum.y * scale, sum.z * scale, sum.w * scale);
+  }
 }
 
 template <int DH>
-__global__ __launch_bounds__(kGradThreads, 1) void grad_kv_plain_kernel(GradParams p, int n_nug_tiles, int n_loc_tiles) {
-  __shared__ float lds[DH / 32 * 16 * kWave];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id(), n = lane & 31, g = lane >> 5;
-  const KeyTile t = key_tile(p, blockIdx.x, n_nug_tiles, n_loc_tiles, 32);
+__global__ __launch_bounds__(kGradThreads, 2) void grad_kv_plain_kernel(GradParams p, int n_nug_tiles, int n_loc_tiles) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id(), n = lane & 15, g = lane >> 4;
+  const KeyTile t = key_tile(p, blockIdx.x, n_nug_tiles, n_loc_tiles, kPlainRows);
   if (t.rows <= 0) return;
-  const int64_t row = t.first + min(n, t.rows - 1);
-  const int64_t off = row * t.tok_stride + t.kvh * t.head_stride;
-  float kf[DH / 2], vf[DH / 2];
+  const int64_t off = (t.first + min(n, t.rows - 1)) * t.tok_stride + t.kvh * t.head_stride;
+  float kf[DH / 4], vf[DH / 4];
   load_row<DH>(t.K, off + 4 * g, kf);
   load_row<DH>(t.V, off + 4 * g, vf);
   OutBlocks<DH> dk, dv;
   clear<DH>(dk);
   clear<DH>(dv);
   const int G = p.H / p.H_kv;
-  for (int e = t.entry0; e < t.entry1; ++e) {
-    const SeenBy s = seen_by(p, t, e, 32);
-    if (!s.any) continue;
-    const int least = s.least(static_cast<int>(t.first - s.key0) + n, n < t.rows);  // first query row that sees this lane's key
-    for (int hg = 0; hg < G; ++hg) {
-      const int h = t.kvh * G + hg;
-      const int64_t stat = static_cast<int64_t>(h) * p.Sq + s.q0;
-      for (int i0 = s.first_row / 32 * 32 + 32 * wave; i0 < s.q_b; i0 += 32 * kGradWaves) {
-        const int64_t a_off = (static_cast<int64_t>(s.q0 + min(i0 + n, s.q_b - 1)) * p.H + h) * DH + 4 * g;
-        floatx16 ds = dot_rows<DH>(p.Q, a_off, kf), dp = dot_rows<DH>(p.dO, a_off, vf);
-        floatx16 pr;
+  for (int e0 = t.entry0; e0 < t.entry1; e0 += kWave) {  // entries that see any of the keys are looked for 64 at a time
+    SeenBy of_lane = {};
+    if (e0 + lane < t.entry1) of_lane = seen_by(p, t, e0 + lane, kPlainRows);
+    for (uint64_t todo = __ballot(of_lane.any && of_lane.first_row < of_lane.q_b); todo != 0; todo &= todo - 1) {
+      const int from = __ffsll(static_cast<long long>(todo)) - 1;
+      SeenBy s;
+      s.q0 = __builtin_amdgcn_readlane(of_lane.q0, from);
+      s.q_b = __builtin_amdgcn_readlane(of_lane.q_b, from);
+      s.key0 = __builtin_amdgcn_readlane(of_lane.key0, from);
+      s.len = __builtin_amdgcn_readlane(of_lane.len, from);
+      s.lag = __builtin_amdgcn_readlane(of_lane.lag, from);
+      s.first_row = __builtin_amdgcn_readlane(of_lane.first_row, from);
+      const int least = s.least(static_cast<int>(t.first - s.key0) + n, n < t.rows);  // first query row that sees this lane's key
+      for (int hg = 0; hg < G; ++hg) {
+        const int h = t.kvh * G + hg;
+        const int64_t stat = static_cast<int64_t>(h) * p.Sq + s.q0;
+        for (int i0 = s.first_row / 16 * 16 + 16 * wave; i0 < s.q_b; i0 += 16 * kGradWaves) {
+          const int64_t a_off = (static_cast<int64_t>(s.q0 + min(i0 + n, s.q_b - 1)) * p.H + h) * DH + 4 * g;
+          float qa[DH / 4], da[DH / 4], lse2[4];
+          load_row<DH>(p.Q, a_off, qa);
+          load_row<DH>(p.dO, a_off, da);
+          floatx4 pr = {0.f, 0.f, 0.f, 0.f}, ds;  // (dP starts from -D, which saves the subtractions)
+          int64_t r_off[4];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int i = i0 + 8 * (v >> 2) + 4 * g + (v & 3), ic = min(i, s.q_b - 1);
-          const bool vis = i >= least && i < s.q_b;
-          const float w = __builtin_amdgcn_exp2f(ds[v] * p.scale_log2e - p.lse2[stat + ic]);
-          pr[v] = vis ? w : 0.f;
-          ds[v] = vis ? w * (dp[v] + p.neg_d[stat + ic]) : 0.f;
-        }
+          for (int v = 0; v < 4; ++v) {
+            const int ic = min(i0 + 4 * g + v, s.q_b - 1);
+            lse2[v] = p.lse2[stat + ic];
+            ds[v] = p.neg_d[stat + ic];
+            r_off[v] = (static_cast<int64_t>(s.q0 + ic) * p.H + h) * DH + 4 * n;
+          }
+          dot_rows<DH>(qa, da, kf, vf, pr, ds);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int ic = min(i0 + 8 * (v >> 2) + 4 * g + (v & 3), s.q_b - 1);
-          const int64_t r_off = (static_cast<int64_t>(s.q0 + ic) * p.H + h) * DH + n;
+          for (int v = 0; v < 4; ++v) {
+            const int i = i0 + 4 * g + v;
+            const bool vis = i >= least && i < s.q_b;
+            const float w = __builtin_amdgcn_exp2f(fmaf(pr[v], p.scale_log2e, -lse2[v]));
+            pr[v] = vis ? w : 0.f;
+            ds[v] = vis ? w * ds[v] : 0.f;
+          }
 #pragma unroll
-          for (int cb = 0; cb < DH / 32; ++cb) {
-            dv[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(load_elem<DODO_DTYPE_F32>(p.dO, r_off + 32 * cb), pr[v], dv[cb], 0, 0, 0);
-            dk[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(load_elem<DODO_DTYPE_F32>(p.Q, r_off + 32 * cb), ds[v], dk[cb], 0, 0, 0);
+          for (int v = 0; v < 4; ++v) {
+            add_column<DH>(dv, p.dO, r_off[v], pr[v]);
+            add_column<DH>(dk, p.Q, r_off[v], ds[v]);
           }
         }
       }
     }
   }
-  sum_wavefronts<DH>(dk, wave, lane, lds);
-  sum_wavefronts<DH>(dv, wave, lane, lds);
-  if (wave == 0 && n < t.rows) {
-    store_row<DH>(t.dK, off, g, dk, p.scale);
-    store_row<DH>(t.dV, off, g, dv, 1.f);
-  }
+  const bool row_ok = n < t.rows;
+  __shared__ float4 lds[2 * kMeetWords<DH>];
+  put_sums<DH>(lds, wave, lane, dk);
+  put_sums<DH>(lds + kMeetWords<DH>, wave, lane, dv);
+  __syncthreads();
+  store_sums<DH>(lds, wave, lane, t.dK, off, row_ok, p.scale);
+  store_sums<DH>(lds + kMeetWords<DH>, wave, lane, t.dV, off, row_ok, 1.f);
 }
 
 template <int DH>
-__global__ __launch_bounds__(kGradThreads, 1) void grad_q_plain_kernel(GradParams p, int n_blocks) {
-  __shared__ float lds[DH / 32 * 16 * kWave];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id(), n = lane & 31, g = lane >> 5;
+__global__ __launch_bounds__(kGradThreads, 2) void grad_q_plain_kernel(GradParams p, int n_blocks) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id(), n = lane & 15, g = lane >> 4;
   const int blk = blockIdx.x % n_blocks, h = blockIdx.x / n_blocks % p.H, e = blockIdx.x / n_blocks / p.H;
   const Entry s = entry_of(p, e);
-  const int i0 = blk * 32;
+  const int i0 = blk * kPlainRows;
   if (i0 >= s.q_b) return;
+  const bool row_ok = i0 + n < s.q_b;
   const int i = min(i0 + n, s.q_b - 1);
-  const int64_t off = (static_cast<int64_t>(s.q0 + i) * p.H + h) * DH;
-  float qf[DH / 2], df[DH / 2];
+  const int64_t off = (static_cast<int64_t>(s.q0 + i) * p.H + h) * DH, stat = static_cast<int64_t>(h) * p.Sq + s.q0 + i;
+  float qf[DH / 4], df[DH / 4];
   load_row<DH>(p.Q, off + 4 * g, qf);
   load_row<DH>(p.dO, off + 4 * g, df);
-  const float lse2 = p.lse2[static_cast<int64_t>(h) * p.Sq + s.q0 + i], neg_d = p.neg_d[static_cast<int64_t>(h) * p.Sq + s.q0 + i];
+  // D and the log-sum-exp in base 2 of the row, here and for the other kernel; a row that sees nothing (-inf) gets +inf: its
+  // weights are 0
+  float lse2 = p.lse[static_cast<int64_t>(s.q0 + i) * p.H + h] * kLog2e, neg_d = 0.f;
+  if (lse2 == -__builtin_inff()) lse2 = __builtin_inff();
+  {
+    float of[DH / 4];
+    load_row<DH>(p.O, off + 4 * g, of);
+#pragma unroll
+    for (int c = 0; c < DH / 4; ++c) neg_d = fmaf(df[c], of[c], neg_d);
+    float lower, upper;
+    lane_pair<16>(neg_d, lower, upper);
+    neg_d = lower + upper;
+    lane_pair<32>(neg_d, lower, upper);
+    neg_d = -(lower + upper);
+  }
+  if (g == 0 && row_ok && wave == 0) {
+    p.lse2[stat] = lse2;
+    p.neg_d[stat] = neg_d;
+  }
   const int kvh = h / (p.H / p.H_kv);
   const int vis = max(0, min(s.m_b, s.m_b - s.q_b + i + 1));  // local rows that this lane's row sees
-  const int most = max(0, min(s.m_b, s.m_b - s.q_b + min(i0 + 32, s.q_b)));
-  const int n_nug = (s.k_b + 31) / 32, n_tiles = n_nug + (most + 31) / 32;
+  const int most = max(0, min(s.m_b, s.m_b - s.q_b + min(i0 + 16, s.q_b)));
+  const int n_nug = (s.k_b + 15) / 16, n_tiles = n_nug + (most + 15) / 16;
   OutBlocks<DH> dq;
   clear<DH>(dq);
   for (int tile = wave; tile < n_tiles; tile += kGradWaves) {
     const bool nug = tile < n_nug;
-    const int j0 = 32 * (nug ? tile : tile - n_nug), len = nug ? s.k_b : most, seen = nug ? s.k_b : vis;
+    const int j0 = 16 * (nug ? tile : tile - n_nug), len = nug ? s.k_b : most, seen = nug ? s.k_b : vis;
     const void *K = nug ? p.Kn : p.Kl, *V = nug ? p.Vn : p.Vl;
     const int64_t tok = nug ? p.nug_tok_stride : p.loc_tok_stride;
-    const int64_t first = (nug ? s.k0 : s.l0) * tok + kvh * (nug ? p.nug_head_stride : DH);
+    const int64_t first = (nug ? s.k0 : s.l0) * tok + kvh * (nug ? p.nug_head_stride : p.loc_head_stride);
     const int64_t a_off = first + min(j0 + n, len - 1) * tok + 4 * g;
-    floatx16 ds = dot_rows<DH>(K, a_off, qf), dp = dot_rows<DH>(V, a_off, df);
+    float ka[DH / 4], va[DH / 4];
+    load_row<DH>(K, a_off, ka);
+    load_row<DH>(V, a_off, va);
+    floatx4 sc = {0.f, 0.f, 0.f, 0.f}, dp = {neg_d, neg_d, neg_d, neg_d};  // (dP starts from -D, which saves the subtractions)
+    dot_rows<DH>(ka, va, qf, df, sc, dp);
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int j = j0 + 8 * (v >> 2) + 4 * g + (v & 3);
-      const float w = __builtin_amdgcn_exp2f(ds[v] * p.scale_log2e - lse2);
-      ds[v] = j < seen ? w * (dp[v] + neg_d) : 0.f;
-    }
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int64_t r_off = first + min(j0 + 8 * (v >> 2) + 4 * g + (v & 3), len - 1) * tok + n;
-#pragma unroll
-      for (int cb = 0; cb < DH / 32; ++cb)
-        dq[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(load_elem<DODO_DTYPE_F32>(K, r_off + 32 * cb), ds[v], dq[cb], 0, 0, 0);
+    for (int v = 0; v < 4; ++v) {
+      const int j = j0 + 4 * g + v;
+      const float ds = __builtin_amdgcn_exp2f(fmaf(sc[v], p.scale_log2e, -lse2)) * dp[v];
+      add_column<DH>(dq, K, first + min(j, len - 1) * tok + 4 * n, j < seen ? ds : 0.f);
     }
   }
-  sum_wavefronts<DH>(dq, wave, lane, lds);
-  if (wave == 0 && i0 + n < s.q_b) store_row<DH>(p.dQ, off, g, dq, p.scale);
+  __shared__ float4 lds[kMeetWords<DH>];
+  put_sums<DH>(lds, wave, lane, dq);
+  __syncthreads();
+  store_sums<DH>(lds, wave, lane, p.dQ, off, row_ok, p.scale);
 }
 
 template <int DH>
 int launch_plain(const GradParams& p) {
-  // one workgroup per 32 keys: of every sequence, or of all rows where entries share them
+  const int64_t blocks = (static_cast<int64_t>(p.max_q) + kPlainRows - 1) / kPlainRows, rows = blocks * p.H * p.B;
+  // keys of every sequence, or of all rows where entries share them
   const int64_t nug_rows = p.shared ? p.Kt : p.max_k, loc_rows = p.shared ? p.Sm : p.max_local;
-  const int64_t nug = (nug_rows + 31) / 32, loc = (loc_rows + 31) / 32;
-  const int64_t owners = (nug + loc) * p.H_kv * (p.shared ? 1 : p.B);
-  const int64_t blocks = (static_cast<int64_t>(p.max_q) + 31) / 32, rows = blocks * p.H * p.B;
-  if (owners > 0x7fffffffLL || rows > 0x7fffffffLL) return DODO_ERR_UNSUPPORTED;
-  if (owners > 0) {
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(grad_kv_plain_kernel<DH>), dim3(static_cast<unsigned>(owners)), dim3(kGradThreads), 0,
-                       p.stream, p, static_cast<int>(nug), static_cast<int>(loc));
+  const int64_t nug = (nug_rows + kPlainRows - 1) / kPlainRows, loc = (loc_rows + kPlainRows - 1) / kPlainRows;
+  const int64_t tiles = (nug + loc) * p.H_kv * (p.shared ? 1 : p.B);
+  if (tiles > 0x7fffffffLL || rows > 0x7fffffffLL) return DODO_ERR_UNSUPPORTED;
+  if (rows > 0) {  // (first: it makes the rows' statistics)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(grad_q_plain_kernel<DH>), dim3(static_cast<unsigned>(rows)), dim3(kGradThreads), 0, p.stream, p,
+                       static_cast<int>(blocks));
     const int rc = launch_status();
     if (rc != DODO_OK) return rc;
   }
-  if (rows == 0) return DODO_OK;
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(grad_q_plain_kernel<DH>), dim3(static_cast<unsigned>(rows)), dim3(kGradThreads), 0, p.stream,
-                     p, static_cast<int>(blocks));
+  if (tiles == 0) return DODO_OK;
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(grad_kv_plain_kernel<DH>), dim3(static_cast<unsigned>(tiles)), dim3(kGradThreads), 0, p.stream, p,
+                     static_cast<int>(nug), static_cast<int>(loc));
   return launch_status();
 }
 
@@ -264,12 +281,6 @@ int grad_entry(GradParams& p, int32_t d_h, int dtype, int layout, void* ws, size
   p.lse2 = static_cast<float*>(ws);
   p.neg_d = p.lse2 + p.Sq * p.H;
   if (dtype == DODO_DTYPE_BF16) return launch_grad_mfma(p, d_h);
-  if (p.max_q > 0) {
-    hipLaunchKernelGGL(grad_rows_kernel, dim3(static_cast<unsigned>((p.Sq * p.H * 16 + 255) / 256)), dim3(256), 0, p.stream,
-                       static_cast<const float*>(p.dO), static_cast<const float*>(p.O), p.lse, p.Sq, p.H, d_h, p.lse2, p.neg_d);
-    const int rc = launch_status();
-    if (rc != DODO_OK) return rc;
-  }
   return d_h == 128 ? launch_plain<128>(p) : launch_plain<64>(p);
 }
 
