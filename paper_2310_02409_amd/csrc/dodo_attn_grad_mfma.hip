@@ -38,11 +38,10 @@ struct TileDims {
 
 // A wavefront's part of the direct loads of a tile of rows `stride` bytes apart: through a buffer that ends with the last
 // valid row (rows beyond read as zeros).
-template <int DH, int NW>
+template <int DH>
 struct TileLoader {
   using TD = TileDims<DH>;
-  static constexpr int kInstr = kTile / TD::kRowsPerInstr / NW;  // direct loads per wavefront, tile and tensor
-  static_assert(kInstr > 0, "every wavefront brings part of a tile");
+  static constexpr int kInstr = kTile / TD::kRowsPerInstr / kGradWaves;  // direct loads per wavefront, tile and tensor
   uint32_t voff[kInstr], lds_off;
   __device__ __forceinline__ void init(int wave, int lane, uint32_t stride) {
     const int row0 = wave * kInstr * TD::kRowsPerInstr + lane / TD::kPieces, pos = lane % TD::kPieces;
@@ -138,12 +137,10 @@ __device__ __forceinline__ void store_rows(char* lds, uint16_t* to, uint32_t str
 }
 
 // ---- dK, dV ------------------------------------------------------------------------------------------------------------
-// A wavefront owns 32 keys, a workgroup 128; its wavefronts walk over the query rows together.  PARTS = 2: eight wavefronts, two per 32
-// keys, one for either half of a tile's rows, whose sums meet in LDS at the end.
+// A wavefront owns 32 keys, a workgroup 128 (BLOCKS = 4); its wavefronts walk over the query rows together.  BLOCKS = 2: 64 keys, two
+// wavefronts per 32, one for either half of a tile's rows, whose sums meet in LDS at the end.
 
-constexpr int kKeys = 32 * kGradWaves;
-
-// A tile of query rows: 64 rows from i0 on of an entry, of head h.
+// A tile of query rows: those from i0 on of an entry, of its K/V head's query head hg.
 struct RowTile {
   int q0, q_b, i0, hg, key0, len, lag;
   bool valid;
@@ -151,9 +148,10 @@ struct RowTile {
 
 // SHARED: entries may share rows, and those that hold any of the workgroup's keys are looked for, 64 at a time; else the keys are
 // those of one entry.
-template <int DH, int PARTS, bool SHARED>
-__global__ __launch_bounds__(PARTS * kGradThreads, PARTS == 1 ? 2 : 1) void grad_kv_kernel(GradParams p, int n_nug_tiles, int n_loc_tiles) {
+template <int DH, int BLOCKS, bool SHARED>
+__global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, int n_nug_tiles, int n_loc_tiles) {
   using TD = TileDims<DH>;
+  constexpr int kParts = kGradWaves / BLOCKS, kKeys = 32 * BLOCKS;
   constexpr int kStage = 2 * TD::kBytes + kTile * 8;  // Q, dO, then log-sum-exp (base 2) and -D of the rows
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
@@ -168,13 +166,13 @@ __global__ __launch_bounds__(PARTS * kGradThreads, PARTS == 1 ? 2 : 1) void grad
   if (t.rows <= 0) return;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & 31, g = lane >> 5;
   const int G = p.H / p.H_kv;
-  const int blk = wave % kGradWaves, part = wave / kGradWaves;
+  const int blk = wave % BLOCKS, part = wave / BLOCKS;
   const int my_rows = min(32, t.rows - blk * 32);  // of this wavefront
   const bool active = my_rows > 0;
   const int64_t my_first = t.first + blk * 32;
 
   const uint32_t row_stride = static_cast<uint32_t>(p.H) * TD::kRowBytes;  // bytes between query rows
-  TileLoader<DH, PARTS * kGradWaves> loader;
+  TileLoader<DH> loader;
   loader.init(wave, lane, row_stride);
   TileReader<DH> reader;
   reader.init(lane);
@@ -282,7 +280,7 @@ __global__ __launch_bounds__(PARTS * kGradThreads, PARTS == 1 ? 2 : 1) void grad
       }
       if (active) {
 #pragma unroll 1
-        for (int hf = part; hf < 2; hf += PARTS) {
+        for (int hf = part; hf < 2; hf += kParts) {
           const int i0 = cur.i0 + 32 * hf;
           if (i0 >= cur.q_b || i0 + 32 <= from) continue;
           const char *qt = base, *dt = base + TD::kBytes;
@@ -354,10 +352,10 @@ __global__ __launch_bounds__(PARTS * kGradThreads, PARTS == 1 ? 2 : 1) void grad
     }
     e0 += kWave;
   } while (SHARED && e0 < t.entry1);
-  if constexpr (PARTS == 2) {
-    constexpr int kRegs = DH / 32 * 16;  // per lane and tensor
-    float* meet = reinterpret_cast<float*>(lds) + blk * 2 * kRegs * kWave + lane;
-    __syncthreads();  // the stages have been read
+  __syncthreads();  // the stages have been read
+  constexpr int kRegs = DH / 32 * 16;  // per lane and tensor
+  if constexpr (kParts == 2) {
+    float* const meet = reinterpret_cast<float*>(lds) + blk * 2 * kRegs * kWave + lane;
     if (part == 1)
 #pragma unroll
       for (int c = 0; c < kRegs; ++c) {
@@ -372,21 +370,19 @@ __global__ __launch_bounds__(PARTS * kGradThreads, PARTS == 1 ? 2 : 1) void grad
       dv[c / 16][c % 16] += meet[(kRegs + c) * kWave];
     }
   }
-  if (PARTS == 1) __syncthreads();  // the stages have been read (two parts: a wavefront's sums are its own)
   if (!active) return;
-  char* out = lds + blk * (PARTS == 2 ? 2 * DH / 32 * 16 * kWave * 4 : kRowsOut<DH>);
+  char* out = lds + blk * (kParts > 1 ? 2 * kRegs * kWave * 4 : kRowsOut<DH>);  // (where it met the others' sums, or a part of the stages)
   const int64_t to = my_first * t.tok_stride + t.kvh * t.head_stride;
   store_rows<DH>(out, static_cast<uint16_t*>(t.local ? p.dKl : p.dKn) + to, static_cast<uint32_t>(t.tok_stride * 2), my_rows, dk, p.scale);
   store_rows<DH>(out, static_cast<uint16_t*>(t.local ? p.dVl : p.dVn) + to, static_cast<uint32_t>(t.tok_stride * 2), my_rows, dv, 1.f);
 }
 
 // ---- dQ ----------------------------------------------------------------------------------------------------------------
-// A wavefront owns 32 query rows of a head; the workgroup's four walk over the keys together: nuggets, then local rows up to the
-// last one that the workgroup's last row sees.
-constexpr int kQueryRows = 32 * kGradWaves;
-
-template <int DH>
+// A wavefront owns 32 query rows of a head, a workgroup 128 (BLOCKS = 4); its wavefronts walk over the keys together: nuggets, then
+// local rows up to the last one that the workgroup's last row sees.  BLOCKS = 2: 64 rows, two wavefronts per 32, as above.
+template <int DH, int BLOCKS>
 __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, int n_blocks) {
+  constexpr int kParts = kGradWaves / BLOCKS, kQueryRows = 32 * BLOCKS;
   using TD = TileDims<DH>;
   constexpr int kStage = 2 * TD::kBytes;  // K, V
   constexpr int kAhead = 2;               // steps that fragments are requested ahead
@@ -400,11 +396,11 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
   if (i0 >= s.q_b) return;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & 31, g = lane >> 5;
   const int kvh = h / (p.H / p.H_kv);
-  const int w_i0 = i0 + 32 * wave;
+  const int blk = wave % BLOCKS, part = wave / BLOCKS, w_i0 = i0 + 32 * blk;
   const bool active = w_i0 < s.q_b, row_ok = w_i0 + n < s.q_b;
   const int i = min(w_i0 + n, s.q_b - 1);
   const int64_t off = (static_cast<int64_t>(s.q0 + i) * p.H + h) * DH;
-  TileLoader<DH, kGradWaves> loader;
+  TileLoader<DH> loader;
   uint32_t loader_stride = 0;
   TileReader<DH> reader;
   reader.init(lane);
@@ -450,7 +446,7 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
   float lower, upper;
   lane_pair<32>(st.y, lower, upper);
   st.y = -(lower + upper);
-  if (g == 0 && row_ok) {
+  if (g == 0 && row_ok && part == 0) {
     p.lse2[static_cast<int64_t>(h) * p.Sq + s.q0 + i] = st.x;
     p.neg_d[static_cast<int64_t>(h) * p.Sq + s.q0 + i] = st.y;
   }
@@ -475,7 +471,7 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
     const int most = (nug ? s.k_b : w_most) - j0, least = (nug ? s.k_b : w_least) - j0;  // ... by some and by all rows of the wavefront
     const char *kt = lds + stage * kStage, *vt = kt + TD::kBytes;
 #pragma unroll 1
-    for (int hf = 0; hf < 2; ++hf) {
+    for (int hf = part; hf < 2; hf += kParts) {
       if (32 * hf >= most) break;
       floatx16 sc = zero16(), dp = neg_d;
       {
@@ -516,48 +512,67 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
     }
   }
   __syncthreads();  // the stages have been read
+  constexpr int kRegs = DH / 32 * 16;  // per lane
+  if constexpr (kParts == 2) {
+    float* const meet = reinterpret_cast<float*>(lds) + blk * kRegs * kWave + lane;
+    if (part == 1)
+#pragma unroll
+      for (int c = 0; c < kRegs; ++c) meet[c * kWave] = dq[c / 16][c % 16];
+    __syncthreads();
+    if (part == 1) return;
+#pragma unroll
+    for (int c = 0; c < kRegs; ++c) dq[c / 16][c % 16] += meet[c * kWave];
+  }
   if (!active) return;
-  store_rows<DH>(lds + wave * kRowsOut<DH>, static_cast<uint16_t*>(p.dQ) + (static_cast<int64_t>(s.q0 + w_i0) * p.H + h) * DH,
+  char* const out = lds + blk * (kParts == 2 ? kRegs * kWave * 4 : kRowsOut<DH>);  // (where it met the other's sums, or a part of the stages)
+  store_rows<DH>(out, static_cast<uint16_t*>(p.dQ) + (static_cast<int64_t>(s.q0 + w_i0) * p.H + h) * DH,
                  static_cast<uint32_t>(p.H) * TD::kRowBytes, min(32, s.q_b - w_i0), dq, p.scale);
 }
 
 static_assert(kGradWaves * kRowsOut<128> <= 2 * 2 * TileDims<128>::kBytes && kGradWaves * kRowsOut<64> <= 2 * 2 * TileDims<64>::kBytes,
               "the stages have room for the rows on their way out");
 
-template <int DH, int PARTS, bool SHARED>
+template <int DH, int BLOCKS, bool SHARED>
 int launch_kv(const GradParams& p) {
-  constexpr int kStages = 2 * (2 * TileDims<DH>::kBytes + kTile * 8) + (SHARED ? 6 * kWave * 4 : 0);
-  constexpr int kMeet = kKeys * DH * 4 * 2;
-  constexpr int kLds = PARTS == 2 && kMeet > kStages ? kMeet : kStages;
+  constexpr int kKeys = 32 * BLOCKS;
+  constexpr int kLds = 2 * (2 * TileDims<DH>::kBytes + kTile * 8) + (SHARED ? 6 * kWave * 4 : 0);
+  static_assert(BLOCKS == 4 || kKeys * DH * 4 * 2 <= kLds, "the stages have room for the sums that meet");
   const int64_t nug_rows = p.shared ? p.Kt : p.max_k, loc_rows = p.shared ? p.Sm : p.max_local;
   const int64_t nug = (nug_rows + kKeys - 1) / kKeys, loc = (loc_rows + kKeys - 1) / kKeys;
   const int64_t owners = (static_cast<int64_t>(p.H_kv) * (p.shared ? 1 : p.B) + 7) / 8 * 8;
   if ((nug + loc) * owners > 0x7fffffffLL) return DODO_ERR_UNSUPPORTED;
   if (nug + loc == 0) return DODO_OK;
-  if constexpr (PARTS == 1) {
-    // Eight wavefronts per 128 keys where the workgroups leave compute units idle and walk over many tiles (the sums' meeting costs
-    // some 5 us).  Four / eight, rows, heads over K/V heads, nuggets, local rows: 1 x 512, 64 over 8, 410, 640 128 / 99 us; 4 x 512
-    // 192 / 153; 1 x 1000, 32 over 8, 1000, 1000 134 / 103; 1 x 2048, 8 over 8, 410, 2048 71 / 59; 5 x 500, 64 over 8, 300, 533 195 /
-    // 200; 1 x 512, 32 over 32, 410, 640 37.5 / 40.8; 8 x 512 160 / 229.
-    const int64_t walked = static_cast<int64_t>(p.H / p.H_kv) * ((p.max_q + kTile - 1) / kTile);
-    if ((nug + loc) * owners < 2 * compute_units() && walked >= 16) return launch_kv<DH, 2, SHARED>(p);
+  if constexpr (BLOCKS == 4) {
+    // 64 keys per workgroup where 128 leave compute units without two of them.  128 / 64 keys, us: 1 sequence of 512 rows, 32 heads, 410
+    // nuggets, 640 local rows 37.5 / 28.5; 64 heads over 8 130 / 85, 4 sequences of it 190 / 130, 8 254 / 251; 1 of 2048, 8 heads, 410, 2048
+    // 71 / 51; 1 of 1000, 32 heads over 8, 1000, 1000 135 / 89, over 32 62 / 74; 8 of 512, 32 heads, 410, 640 152 / 203; 8 of 16, 100, 32
+    // 11 / 20.  (32 keys, by four wavefronts: 84, 71, 267, 509, 82, 138, 176, 564, 61.)
+    if ((nug + loc) * owners < 2 * compute_units()) return launch_kv<DH, 2, SHARED>(p);
   }
-  const auto kern = grad_kv_kernel<DH, PARTS, SHARED>;
+  const auto kern = grad_kv_kernel<DH, BLOCKS, SHARED>;
   const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kern), kLds);
   if (rc != DODO_OK) return rc;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((nug + loc) * owners)), dim3(PARTS * kGradThreads), kLds, p.stream, p, static_cast<int>(nug),
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((nug + loc) * owners)), dim3(kGradThreads), kLds, p.stream, p, static_cast<int>(nug),
                      static_cast<int>(loc));
   return launch_status();
 }
 
-template <int DH>
+template <int DH, int BLOCKS>
 int launch_q(const GradParams& p) {
+  constexpr int kQueryRows = 32 * BLOCKS;
   constexpr int kLds = 2 * 2 * TileDims<DH>::kBytes;
+  static_assert(kQueryRows * DH * 4 <= kLds, "the stages have room for the sums that meet");
   const int64_t blocks = (static_cast<int64_t>(p.max_q) + kQueryRows - 1) / kQueryRows;
   const int64_t owners = (static_cast<int64_t>(p.H) * p.B + 7) / 8 * 8;
   if (blocks * owners > 0x7fffffffLL) return DODO_ERR_UNSUPPORTED;
   if (blocks * owners == 0) return DODO_OK;
-  const auto kern = grad_q_kernel<DH>;
+  if constexpr (BLOCKS == 4) {
+    // 64 rows per workgroup where 128 leave compute units idle or barely fill them.  128 / 64 rows, us: 1 sequence of 512 rows, 32 heads,
+    // 410 nuggets, 640 local rows 33 / 24, 64 heads 36 / 36, 2 sequences of 32 heads 36 / 36, of 64 56 / 64; 1 of 2048, 8 heads, 410, 2048
+    // 64 / 43; 1 of 64, 32 heads, 3277, 128 81 / 54; 8 of 64, 410, 128 20.9 / 18.8; 8 of 512, 410, 640 115 / 134.
+    if (blocks * owners <= compute_units()) return launch_q<DH, 2>(p);
+  }
+  const auto kern = grad_q_kernel<DH, BLOCKS>;
   const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kern), kLds);
   if (rc != DODO_OK) return rc;
   hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(blocks * owners)), dim3(kGradThreads), kLds, p.stream, p, static_cast<int>(blocks));
@@ -566,9 +581,9 @@ int launch_q(const GradParams& p) {
 
 template <int DH>
 int launch_both(const GradParams& p) {
-  const int rc = launch_q<DH>(p);  // (first: it makes the rows' statistics)
+  const int rc = launch_q<DH, 4>(p);  // (first: it makes the rows' statistics)
   if (rc != DODO_OK) return rc;
-  return p.shared ? launch_kv<DH, 1, true>(p) : launch_kv<DH, 1, false>(p);
+  return p.shared ? launch_kv<DH, 4, true>(p) : launch_kv<DH, 4, false>(p);
 }
 
 }  // namespace
