@@ -1,7 +1,7 @@
 // dodo_nugget_attention_q4: nugget attention (Eq. 13 / Eq. 9 of the Dodo paper) over a nugget cache held in 4 bits.
 //
 // Few query rows (bf16): one kernel reads the codes where they are, a quarter of a bf16 cache's bytes, and every one once for
-// 16 or 32 query vectors.  A workgroup owns a share of the keys of one (sequence, K/V head, group of query rows); each of its four
+// 16 or 32 query vectors.  A workgroup owns a share of the keys of one (sequence, K/V head, group of query rows); each of its four or eight
 // wavefronts takes tiles of 32 keys of it, without a barrier in the loop:
 //   K      codes go straight to registers: the sum over channels may run in any order, so a lane takes consecutive channels of
 //          its key, whose codes are one load and whose scale is one byte (two bytes for 64 channels), and the query vectors'
@@ -25,8 +25,6 @@ namespace dodo {
 namespace {
 
 constexpr int kKeysQ4 = 32;                 // keys per tile
-constexpr int kWavesQ4 = 4;
-constexpr int kThreadsQ4 = kWavesQ4 * kWave;
 constexpr int kVectorsQ4 = 32;              // query vectors per workgroup at most
 constexpr int kCounters = DODO_Q4_ZEROED_BYTES / 4;  // words at the workspace's start, one per (sequence, K/V head, group of query rows)
 constexpr int kMaxSplitsQ4 = 32;
@@ -50,8 +48,8 @@ struct Q4Dims {
   static constexpr int kPartBytes = (NV * kPartStride + 2 * NV) * 4;
   static constexpr int kWaveLds = ((2 * kTensorBytes > kPartBytes ? 2 * kTensorBytes : kPartBytes) + 1023) / 1024 * 1024;
   static constexpr int kQBytes = NV * kRowBytes;
-  static constexpr int kLds = kWavesQ4 * kWaveLds + kQBytes;
-  static_assert(2 * kLds <= 160 * 1024, "two workgroups on a compute unit");
+  static constexpr int lds_bytes(int waves) { return waves * kWaveLds + kQBytes; }
+  static_assert(2 * lds_bytes(4) <= 160 * 1024 && lds_bytes(8) <= 160 * 1024, "two workgroups of four wavefronts on a compute unit, or one of eight");
   static_assert((2 * NV * kMaxSplitsQ4 + 3 * NV) * 4 <= kWaveLds, "the merge's staging fits into a wavefront's LDS");
 };
 
@@ -91,8 +89,8 @@ __device__ __forceinline__ Codes<N> load_codes(const uint8_t* p) {
   }
   return c;
 }
-template <int DH, int NV>
-__global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
+template <int DH, int NV, int NW>
+__global__ __launch_bounds__(NW * kWave, 2) void attention_q4_kernel(Q4Args a) {
   using QD = Q4Dims<DH, NV>;
   using Acc = typename Mfma<NV>::Acc;
   constexpr int kRowBytes = QD::kRowBytes, kP = QD::kP, kRowShift = QD::kRowShift, kCB = QD::kCB, kSteps = QD::kSteps;
@@ -128,7 +126,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
   const int nug_end = min(t1, n_nug);
   // tiles t0 + wave, t0 + wave + 4, ...: first nuggets, then (from local tile l_first on) local rows
   const int first = t0 + wave;
-  const int skip = first < n_nug ? (n_nug - first + kWavesQ4 - 1) / kWavesQ4 * kWavesQ4 : 0;
+  const int skip = first < n_nug ? (n_nug - first + NW - 1) / NW * NW : 0;
   const int l_first = first + skip - n_nug, l_end_tile = t1 - n_nug;
 
   char* const lds_w = lds + wave * kWaveLds;
@@ -158,7 +156,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
 
   // The query vectors go through LDS; every wavefront brings a part of them.
   {
-    constexpr int kQInstr = (QD::kQBytes / 1024 + kWavesQ4 - 1) / kWavesQ4;
+    constexpr int kQInstr = (QD::kQBytes / 1024 + NW - 1) / NW;
     const u32x4_t qbuf = buffer_of(a.Q + (static_cast<int64_t>(q0 + row0) * a.H + kvh * G) * DH, 0xffffffffu);
 #pragma unroll
     for (int u = 0; u < kQInstr; ++u) {
@@ -166,7 +164,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
       const int v = chunk * kRowsPerInstr + ld_row0, jv = v < nv ? v : 0;  // spare rows repeat vector 0; nothing of them is stored
       const int il = static_cast<int>(fast_div(static_cast<uint32_t>(jv), a.div_G));
       dma16_buffer(qbuf, static_cast<uint32_t>(il * a.H + jv - il * G) * kRowBytes + k_piece_of(v),
-                   __builtin_amdgcn_readfirstlane(lds_addr + kWavesQ4 * kWaveLds + chunk * 1024));
+                   __builtin_amdgcn_readfirstlane(lds_addr + NW * kWaveLds + chunk * 1024));
     }
   }
   if (l_first < l_end_tile) issue_local(l_first, IsK{});  // (nuggets' K does not touch that half)
@@ -204,12 +202,12 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
   Tile buf[kTilesAhead + 1];
 #pragma unroll
   for (int c = 0; c < kTilesAhead; ++c)
-    if (first + c * kWavesQ4 < nug_end) buf[c] = load_tile(first + c * kWavesQ4);
+    if (first + c * NW < nug_end) buf[c] = load_tile(first + c * NW);
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   __syncthreads();  // every wavefront's part of the query vectors has landed
   bf16x8 qf[kSteps];  // lane (j, g): channels kRun g + 8 ds .. + 8 of its vector
   {
-    const char* q_lds = lds + kWavesQ4 * kWaveLds + j * kRowBytes;
+    const char* q_lds = lds + NW * kWaveLds + j * kRowBytes;
 #pragma unroll
     for (int ds = 0; ds < kSteps; ++ds)
       qf[ds] = *reinterpret_cast<const bf16x8*>(q_lds + (((kSteps * g + ds) ^ ((j >> kRowShift) & (kP - 1))) << 4));
@@ -290,10 +288,10 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
     read_v(vt);
     add_v(vt, pf);
   };
-  for (int t = first; t < nug_end; t += (kTilesAhead + 1) * kWavesQ4) {
+  for (int t = first; t < nug_end; t += (kTilesAhead + 1) * NW) {
 #pragma unroll
     for (int c = 0; c <= kTilesAhead; ++c) {  // (every buffer has its registers: a copy would wait for the tile)
-      const int now = t + c * kWavesQ4, then = now + kTilesAhead * kWavesQ4;
+      const int now = t + c * NW, then = now + kTilesAhead * NW;
       if (now >= nug_end) break;
       if (then < nug_end) buf[(c + kTilesAhead) % (kTilesAhead + 1)] = load_tile(then);
       nugget_tile(now, buf[c]);
@@ -305,8 +303,8 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
     __builtin_amdgcn_sched_barrier(0);
     issue_local(l_first, IsV{});
   }
-  for (int t = l_first; t < l_end_tile; t += kWavesQ4) {
-    const bool more = t + kWavesQ4 < l_end_tile;
+  for (int t = l_first; t < l_end_tile; t += NW) {
+    const bool more = t + NW < l_end_tile;
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(kInstr));  // K has landed, V may be in flight
     asm volatile("" ::: "memory");
     bf16x8 kf[QD::kKeyBlocks][kSteps];
@@ -317,7 +315,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
         kf[kb][ds] = *reinterpret_cast<const bf16x8*>(kbuf + (NV * kb + j) * kRowBytes + (((kSteps * g + ds) ^ (((NV * kb + j) >> kRowShift) & (kP - 1))) << 4));
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
     __builtin_amdgcn_sched_barrier(0);
-    if (more) issue_local(t + kWavesQ4, IsK{});
+    if (more) issue_local(t + NW, IsK{});
     __builtin_amdgcn_sched_barrier(0);
     Acc acc_s[QD::kKeyBlocks];
     clear(acc_s);
@@ -336,7 +334,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
     read_v(vt);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
     __builtin_amdgcn_sched_barrier(0);
-    if (more) issue_local(t + kWavesQ4, IsV{});
+    if (more) issue_local(t + NW, IsV{});
     __builtin_amdgcn_sched_barrier(0);
     add_v(vt, pf);
   }
@@ -361,17 +359,17 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
   // Four neighbouring channels of a vector, the wavefronts merged in wavefront order.  A part without keys has m = -inf, a sum of 0 and
   // channels 0; one whose logits are NaN may have m = -inf as well, but its sum is NaN and stays so.
   auto merged = [&](int v, int c, float& M, float& S, float4& o) {
-    float mw[kWavesQ4];
+    float mw[NW];
     M = kNegInf;
 #pragma unroll
-    for (int w = 0; w < kWavesQ4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       mw[w] = reinterpret_cast<const float*>(lds + w * kWaveLds)[NV * kPartStride + v];
       M = fmaxf(M, mw[w]);
     }
     S = 0.f;
     o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < kWavesQ4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float* part = reinterpret_cast<const float*>(lds + w * kWaveLds);
       const float wgt = exp2_hw(mw[w] - (M == kNegInf ? 0.f : M));
       S = fmaf(part[NV * kPartStride + NV + v], wgt, S);
@@ -388,7 +386,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
   };
   const int n_quads = nv * (DH / 4);
   if (a.nsplit == 1) {
-    for (int e = tid; e < n_quads; e += kThreadsQ4) {
+    for (int e = tid; e < n_quads; e += NW * kWave) {
       const int v = e / (DH / 4), c = 4 * (e % (DH / 4));
       float M, S;
       float4 o;
@@ -404,7 +402,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
   auto word_of = [](float lo, float hi) -> uint64_t { return static_cast<uint64_t>(__float_as_uint(hi)) << 32 | __float_as_uint(lo); };
   auto lo_of = [](uint64_t w) -> float { return __uint_as_float(static_cast<uint32_t>(w)); };
   auto hi_of = [](uint64_t w) -> float { return __uint_as_float(static_cast<uint32_t>(w >> 32)); };
-  for (int e = tid; e < n_quads; e += kThreadsQ4) {
+  for (int e = tid; e < n_quads; e += NW * kWave) {
     const int v = e / (DH / 4), c = 4 * (e % (DH / 4));
     float M, S;
     float4 o;
@@ -425,7 +423,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
   float* const st_s = st_m + NV * kMaxSplitsQ4;
   float* const tot_s = st_s + NV * kMaxSplitsQ4;
   float* const tot_m = tot_s + NV;
-  for (int f = tid; f < nv * a.nsplit; f += kThreadsQ4) {
+  for (int f = tid; f < nv * a.nsplit; f += NW * kWave) {
     const uint64_t ms = __hip_atomic_load(recs + static_cast<int64_t>(f) * kWords, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     st_m[f] = lo_of(ms);
     st_s[f] = hi_of(ms);
@@ -443,7 +441,7 @@ __global__ __launch_bounds__(kThreadsQ4, 2) void attention_q4_kernel(Q4Args a) {
     tot_m[tid] = M;
   }
   __syncthreads();
-  for (int e = tid; e < n_quads; e += kThreadsQ4) {
+  for (int e = tid; e < n_quads; e += NW * kWave) {
     const int v = e / (DH / 4), c = 4 * (e % (DH / 4));
     const uint64_t* rec = recs + static_cast<int64_t>(v) * a.nsplit * kWords + 1 + c / 2;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -480,7 +478,7 @@ constexpr int kNugCost = 1, kLocCost = 2;
 // How the direct kernel would take a call (bf16, d_h 64 or 128, at most kVectorsQ4 heads per K/V head).
 struct Plan {
   bool direct, narrow;  // narrow: groups of up to 16 vectors
-  int rows_per, n_groups, nsplit;
+  int rows_per, n_groups, nsplit, waves;
   size_t records;  // bytes behind the counters
 };
 Plan plan_of(int64_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int32_t max_k, int32_t max_local, int dtype) {
@@ -493,6 +491,7 @@ Plan plan_of(int64_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int
   if (static_cast<int64_t>(B) * H_kv > 1 << 22) return p;  // (the grid, with up to 32 shares and 15 groups of rows)
   if (static_cast<int64_t>(H) * d_h >= 1 << 24) return p;  // (offsets between rows of a tile in 32 bits)
   p.direct = true;
+  p.waves = 4;
   // Groups of 16 vectors where that leaves no compute unit with more than two workgroups, else of 32, which read the cache half as often.
   // 16 / 32: 8 sequences, 32 heads, 410 nuggets, 257 local rows: 32 rows 17.3 / 22.0 us, 64 rows 30.6 / 22.6; 32 sequences, 32 rows 77.2 / 54.0;
   // 64 heads over 8, 4 rows, 3277 nuggets, 1 sequence 14.9 / 19.7, 8 22.4 / 24.2.
@@ -509,15 +508,23 @@ Plan plan_of(int64_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int
   // us in 28 / 14 / 16 shares, 2 of them with 1089 local rows 18.3 / 13.3 / 13.6 in 32 / 16 / 8, 8 15.4 / 16.6 in 8 / 4; 32 over 32, 410
   // nuggets, 1 sequence 8.7 / 10.6 in 5 / 2, 8 with 4 rows 13.0 / 14.5 in 1 / 2, 16 22.9 / 28.3 in 1 / 2.
   int64_t n = 1, best = 0;
-  for (int64_t s = 1; s <= kMaxSplitsQ4 && (s == 1 || (pairs <= kCounters && s * kWavesQ4 <= cost)); ++s) {
+  for (int64_t s = 1; s <= kMaxSplitsQ4 && (s == 1 || (pairs <= kCounters && s * p.waves <= cost)); ++s) {
     const int64_t workgroups = pairs * s;
     const int64_t tile = (p.narrow ? 900 : 1800) * (workgroups <= cus ? 2 : 3) / 2;
-    const int64_t units = std::max<int64_t>((cost + s * kWavesQ4 - 1) / (s * kWavesQ4), max_local > 0 ? kLocCost : kNugCost);
+    const int64_t units = std::max<int64_t>((cost + s * p.waves - 1) / (s * p.waves), max_local > 0 ? kLocCost : kNugCost);
     const int64_t ns = std::max(units * tile, units * tile * workgroups / (2 * cus)) + (s == 1 ? 0 : 2000 + 13 * s * vectors);
     if (s == 1 || ns < best) {
       n = s;
       best = ns;
     }
+  }
+  // Two shares in one workgroup of eight wavefronts, which meet in LDS instead of memory, where there are many records to merge or at least
+  // four tiles a wavefront.  Four / eight wavefronts, us (64 heads over 8, 3277 nuggets, 257 local rows, unless said): 32 sequences 42.1 /
+  // 40.4, 16 24.8 / 25.0, 8 15.4 / 15.3, of 4 rows 22.6 / 20.3, 2 of 8 rows 17.0 / 15.5; 32 heads over 32 12.6 / 12.0; 2 of 16 rows, 8 heads
+  // of 64 over 2 11.9 / 10.3.  Short: 32 heads, 410 nuggets 8.4 / 10.0; 3 sequences of 500 and 500, 32 heads over 8 8.9 / 10.3.
+  if (n % 2 == 0 && (vectors * n >= 64 || cost >= 16 * n)) {
+    p.waves = 8;
+    n /= 2;
   }
   p.nsplit = static_cast<int>(n);
   p.records = n == 1 ? 0 : static_cast<size_t>(pairs) * p.rows_per * G * n * (d_h + 2) * sizeof(float);
@@ -527,13 +534,19 @@ Plan plan_of(int64_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr size_t kCounterBytes = kCounters * sizeof(uint32_t);
 
-template <int DH, int NV>
+template <int DH, int NV, int NW>
 int launch_direct(const Q4Args& a, hipStream_t stream) {
-  const auto kern = attention_q4_kernel<DH, NV>;
-  const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kern), Q4Dims<DH, NV>::kLds);
+  constexpr int kLds = Q4Dims<DH, NV>::lds_bytes(NW);
+  const auto kern = attention_q4_kernel<DH, NV, NW>;
+  const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kern), kLds);
   if (rc != DODO_OK) return rc;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((a.n_units + 7) / 8 * 8 * a.heads_per_unit)), dim3(kThreadsQ4), (Q4Dims<DH, NV>::kLds), stream, a);
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((a.n_units + 7) / 8 * 8 * a.heads_per_unit)), dim3(NW * kWave), kLds, stream, a);
   return launch_status();
+}
+template <int DH>
+int launch_direct(const Q4Args& a, const Plan& plan, hipStream_t stream) {
+  if (plan.waves == 8) return plan.narrow ? launch_direct<DH, 16, 8>(a, stream) : launch_direct<DH, 32, 8>(a, stream);
+  return plan.narrow ? launch_direct<DH, 16, 4>(a, stream) : launch_direct<DH, 32, 4>(a, stream);
 }
 
 }  // namespace
@@ -591,8 +604,7 @@ extern "C" int dodo_nugget_attention_q4(const void* Q, const uint8_t* Kc, const 
     const auto units = [&]() { return static_cast<int64_t>(B) * plan.nsplit * plan.n_groups * (H_kv / a.heads_per_unit); };
     while (a.heads_per_unit % 2 == 0 && units() % 8 != 0 && units() < 64) a.heads_per_unit /= 2;
     a.n_units = static_cast<int>(units());
-    if (d_h == 128) return plan.narrow ? launch_direct<128, 16>(a, s) : launch_direct<128, 32>(a, s);
-    return plan.narrow ? launch_direct<64, 16>(a, s) : launch_direct<64, 32>(a, s);
+    return d_h == 128 ? launch_direct<128>(a, plan, s) : launch_direct<64>(a, plan, s);
   }
   const size_t attention = dodo_nugget_attention_workspace_bytes_grouped(B, H, H_kv, d_h, max_q, max_k, max_local, dtype);
   const size_t cache = round256(static_cast<size_t>(Kt) * H_kv * d_h * elem_bytes(dtype));
