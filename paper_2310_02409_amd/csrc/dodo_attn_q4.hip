@@ -14,6 +14,11 @@
 // keys are shared out, every workgroup writes its partial results, counts itself, and the last to come merges all of them in
 // order of their shares: nothing waits, and the order of the sums does not depend on who is last.
 //
+// What bounds it: memory where the cache is large (a decode step of 32 ragged sequences, 64 heads over 8, up to 3277 nuggets: 34.4
+// us over fresh caches, 3.5 TB/s; 32 equal ones 40 us, 3.7 TB/s, by heads 33 us, 4.4 TB/s, since token by token a head's codes are half
+// a cache line); a chain of latencies where it is small (1 sequence, 32 heads, 410 nuggets 8.3 us: ranges, queries and codes, a tile or
+// two, the shares' meeting).
+//
 // Many query rows, other types: the cache is unpacked into the workspace and attended over from there.
 #include <algorithm>
 #include <type_traits>
@@ -26,6 +31,7 @@ namespace {
 
 constexpr int kKeysQ4 = 32;                 // keys per tile
 constexpr int kVectorsQ4 = 32;              // query vectors per workgroup at most
+constexpr int kMostVectorsQ4 = 128;         // ... and of a K/V head and sequence, where there are many rows
 constexpr int kCounters = DODO_Q4_ZEROED_BYTES / 4;  // words at the workspace's start, one per (sequence, K/V head, group of query rows)
 constexpr int kMaxSplitsQ4 = 32;
 
@@ -484,10 +490,11 @@ struct Plan {
 Plan plan_of(int64_t B, int32_t H, int32_t H_kv, int32_t d_h, int32_t max_q, int32_t max_k, int32_t max_local, int dtype) {
   Plan p = {};
   const int64_t G = H / H_kv;
-  // Up to 64 vectors a K/V head, and up to 15 rows whatever the heads; beyond, where the vectors read the cache several times, unpacking it
-  // once is the faster.  Here / unpacked, 8 sequences, 32 heads, 410 nuggets, 257 local rows: 16 rows 13.7 / 33.1 us, 32 rows 30.1 / 34.2, 64
-  // rows 34.9 / 35.4, 128 rows 63.2 / 40.7; 32 sequences, 32 rows 71.9 / 121; 64 heads over 8, 3277 nuggets, 16 rows 66.3 / 65.3, 64 rows 191 / 116.
-  if (dtype != DODO_DTYPE_BF16 || G > kVectorsQ4 || (max_q >= DODO_ATTENTION_BLOCK_MIN_Q && max_q * G > 2 * kVectorsQ4)) return p;
+  // Up to 128 vectors a K/V head, and up to 15 rows whatever the heads; beyond, where the vectors read the cache several times, unpacking it
+  // once is the faster.  Here / unpacked, us, 257 local rows: 8 sequences, 32 heads over 32, 410 nuggets, 16 rows 13.8 / 33.6, 64 22.6 / 35.7,
+  // 128 38.5 / 41.6, 256 68.0 / 46.7; 32 sequences, 32 rows 53 / 120, 64 91 / 126, 128 153 / 136; 64 heads over 8, 3277 nuggets, 16 rows 15.1 /
+  // 27.5, 8 sequences of it 44.6 / 63.0.
+  if (dtype != DODO_DTYPE_BF16 || G > kVectorsQ4 || (max_q >= DODO_ATTENTION_BLOCK_MIN_Q && max_q * G > kMostVectorsQ4)) return p;
   if (static_cast<int64_t>(B) * H_kv > 1 << 22) return p;  // (the grid, with up to 32 shares and 15 groups of rows)
   if (static_cast<int64_t>(H) * d_h >= 1 << 24) return p;  // (offsets between rows of a tile in 32 bits)
   p.direct = true;

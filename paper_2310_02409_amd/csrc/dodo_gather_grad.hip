@@ -5,7 +5,8 @@
 // A pass over memory that mostly writes zeros.  Without accumulation a workgroup writes the rows of kTokens consecutive tokens of
 // K or of V: one search in the sequence's ascending list for the first of them, then the list is read on from
 // there, one entry per lane, and a ballot tells each token how many rows are its own.  So no row is written twice and
-// there are no atomics, and a list with repeated indices gives the same sum every time.  With accumulation only
+// there are no atomics, and a list with repeated indices gives the same sum every time.  8 sequences of 4096 tokens at 10x, 32 heads of
+// 128, bf16: 114 us, 5.2 TB/s of the bytes that have to move (a fill reaches 6.9, a copy 4.9); a workgroup per token and tensor took 155.  With accumulation only
 // the nuggets' tokens are touched: one workgroup per cache row, of which the first of a run of equal indices adds the run.
 #include "dodo_lists.h"
 
