@@ -10,7 +10,7 @@
 //
 // What bounds them: a wavefront with 32 owned rows of 128 channels fills its registers, so every matrix instruction comes with 16 bytes a
 // lane from LDS, and LDS is as busy as the matrix pipes; in long calls the card lowers its clock to 1.9 GHz besides.  16 sequences of
-// 2048 rows, 40 heads of 128 (5 products: 1.87 PFLOP): 2.76 ms, 680 TFLOP/s of the 5 products and 950 of the 7 executed, where a large
+// 2048 rows, 40 heads of 128 (5 products: 1.89 TFLOP): 2.76 ms, 680 TFLOP/s of the 5 products and 950 of the 7 executed, where a large
 // library product reaches 1180 to 1360.  (64 owned rows a wavefront, tiles of 128 rows, or the second products one tile later: slower, by
 // spills or by fewer wavefronts.)
 #include <type_traits>
