@@ -44,10 +44,10 @@ struct TileDims {
 
 // A wavefront's part of the direct loads of a tile of rows `stride` bytes apart: through a buffer that ends with the last
 // valid row (rows beyond read as zeros).
-template <int DH>
+template <int DH, int NW = kGradWaves, int ROWS = kTile>
 struct TileLoader {
   using TD = TileDims<DH>;
-  static constexpr int kInstr = kTile / TD::kRowsPerInstr / kGradWaves;  // direct loads per wavefront, tile and tensor
+  static constexpr int kInstr = ROWS / TD::kRowsPerInstr / NW;  // direct loads per wavefront, tile and tensor
   uint32_t voff[kInstr], lds_off;
   __device__ __forceinline__ void init(int wave, int lane, uint32_t stride) {
     const int row0 = wave * kInstr * TD::kRowsPerInstr + lane / TD::kPieces, pos = lane % TD::kPieces;
@@ -143,8 +143,11 @@ __device__ __forceinline__ void store_rows(char* lds, uint16_t* to, uint32_t str
 }
 
 // ---- dK, dV ------------------------------------------------------------------------------------------------------------
-// A wavefront owns 32 keys, a workgroup 128 (BLOCKS = 4); its wavefronts walk over the query rows together.  BLOCKS = 2: 64 keys, two
-// wavefronts per 32, one for either half of a tile's rows, whose sums meet in LDS at the end.
+// A wavefront owns 32 keys, a workgroup 128 (BLOCKS = 4); its wavefronts walk over the query rows together.  BLOCKS = 2: 64 keys, two or
+// four wavefronts (PARTS) per 32, one for either half of a tile's rows, or a quarter of two tiles', whose sums meet in LDS at the end.
+
+template <int PARTS>
+constexpr int kWalked = PARTS == 4 ? 2 * kTile : kTile;  // rows in LDS at a time
 
 // A tile of query rows: those from i0 on of an entry, of its K/V head's query head hg.
 struct RowTile {
@@ -154,11 +157,11 @@ struct RowTile {
 
 // SHARED: entries may share rows, and those that hold any of the workgroup's keys are looked for, 64 at a time; else the keys are
 // those of one entry.
-template <int DH, int BLOCKS, bool SHARED>
-__global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, int n_nug_tiles, int n_loc_tiles) {
+template <int DH, int BLOCKS, int PARTS, bool SHARED>
+__global__ __launch_bounds__(BLOCKS * PARTS * kWave, 2) void grad_kv_kernel(GradParams p, int n_nug_tiles, int n_loc_tiles) {
   using TD = TileDims<DH>;
-  constexpr int kParts = kGradWaves / BLOCKS, kKeys = 32 * BLOCKS;
-  constexpr int kStage = 2 * TD::kBytes + kTile * 8;  // Q, dO, then log-sum-exp (base 2) and -D of the rows
+  constexpr int kKeys = 32 * BLOCKS, kRows = kWalked<PARTS>, kTensor = kRows * TD::kRowBytes;
+  constexpr int kStage = 2 * kTensor + kRows * 8;  // Q, dO, then log-sum-exp (base 2) and -D of the rows
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
   int* const entries = reinterpret_cast<int*>(lds + 2 * kStage);  // (SHARED)
@@ -178,7 +181,7 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, 
   const int64_t my_first = t.first + blk * 32;
 
   const uint32_t row_stride = static_cast<uint32_t>(p.H) * TD::kRowBytes;  // bytes between query rows
-  TileLoader<DH> loader;
+  TileLoader<DH, BLOCKS * PARTS, kRows> loader;
   loader.init(wave, lane, row_stride);
   TileReader<DH> reader;
   reader.init(lane);
@@ -239,29 +242,31 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, 
         r.i0 = __builtin_amdgcn_readfirstlane(of[5 * kWave]);
       }
       todo &= todo - 1;
-      r.i0 = r.i0 / kTile * kTile;
+      r.i0 = r.i0 / kRows * kRows;
       r.hg = 0;
       return r;
     };
     auto first_tile = [&](const RowTile& r) {  // of the entry, for the next head
-      return t.local ? static_cast<int>(max(static_cast<int64_t>(0), max(t.first - r.key0, static_cast<int64_t>(0)) - r.lag)) / kTile * kTile : 0;
+      return t.local ? static_cast<int>(max(static_cast<int64_t>(0), max(t.first - r.key0, static_cast<int64_t>(0)) - r.lag)) / kRows * kRows : 0;
     };
     auto advance = [&](RowTile r) -> RowTile {
-      r.i0 += kTile;
+      r.i0 += kRows;
       if (r.i0 < r.q_b) return r;
       r.i0 = first_tile(r);
       if (++r.hg < G) return r;
       return entry_tile();
     };
     auto issue = [&](const RowTile& r, int stage) {
-      const int h = t.kvh * G + r.hg, rows = min(kTile, r.q_b - r.i0);
+      const int h = t.kvh * G + r.hg, rows = min(kRows, r.q_b - r.i0);
       const int64_t first = (static_cast<int64_t>(r.q0 + r.i0) * p.H + h) * DH;
       const uint32_t dst = lds_base + stage * kStage;
       loader.issue(static_cast<const uint16_t*>(p.Q) + first, rows, row_stride, dst);
-      loader.issue(static_cast<const uint16_t*>(p.dO) + first, rows, row_stride, dst + TD::kBytes);
-      if (wave < 2) {
-        const float* from = (wave == 0 ? p.lse2 : p.neg_d) + static_cast<int64_t>(h) * p.Sq + r.q0 + r.i0;
-        dma4_buffer(buffer_of(from, rows * 4u), lane * 4u, __builtin_amdgcn_readfirstlane(dst + 2 * TD::kBytes + wave * (kTile * 4)));
+      loader.issue(static_cast<const uint16_t*>(p.dO) + first, rows, row_stride, dst + kTensor);
+      if (wave < kRows / 32) {  // 64 of either statistic
+        const int of = wave % 2, first_row = kRows > kTile ? wave / 2 * kTile : 0;
+        const float* from = (of == 0 ? p.lse2 : p.neg_d) + static_cast<int64_t>(h) * p.Sq + r.q0 + r.i0 + first_row;
+        dma4_buffer(buffer_of(from, max(rows - first_row, 0) * 4u), lane * 4u,
+                    __builtin_amdgcn_readfirstlane(dst + 2 * kTensor + (of * kRows + first_row) * 4));
       }
     };
     RowTile cur = entry_tile();
@@ -286,17 +291,17 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, 
       }
       if (active) {
 #pragma unroll 1
-        for (int hf = part; hf < 2; hf += kParts) {
+        for (int hf = part; hf < kRows / 32; hf += PARTS) {
           const int i0 = cur.i0 + 32 * hf;
           if (i0 >= cur.q_b || i0 + 32 <= from) continue;
-          const char *qt = base, *dt = base + TD::kBytes;
-          const float* lse2 = reinterpret_cast<const float*>(base + 2 * TD::kBytes) + 32 * hf + 4 * g;
+          const char *qt = base, *dt = base + kTensor;
+          const float* lse2 = reinterpret_cast<const float*>(base + 2 * kTensor) + 32 * hf + 4 * g;
           // Fragments are requested one step (two matrix instructions) ahead; the scheduling barriers keep the compiler from
           // requesting them all at once, which would not fit into the registers.
           floatx16 s = zero16(), dp;  // (dP starts from -D, which saves the subtractions)
 #pragma unroll
           for (int v4 = 0; v4 < 4; ++v4) {
-            const float4 d = *reinterpret_cast<const float4*>(lse2 + kTile + 8 * v4);
+            const float4 d = *reinterpret_cast<const float4*>(lse2 + kRows + 8 * v4);
             dp[4 * v4] = d.x; dp[4 * v4 + 1] = d.y; dp[4 * v4 + 2] = d.z; dp[4 * v4 + 3] = d.w;
           }
           bf16x8 qa[2], da[2];
@@ -360,24 +365,26 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_kv_kernel(GradParams p, 
   } while (SHARED && e0 < t.entry1);
   __syncthreads();  // the stages have been read
   constexpr int kRegs = DH / 32 * 16;  // per lane and tensor
-  if constexpr (kParts == 2) {
-    float* const meet = reinterpret_cast<float*>(lds) + blk * 2 * kRegs * kWave + lane;
-    if (part == 1)
+  if constexpr (PARTS > 1) {  // dK, then dV: the other parts' sums, added in their order
+    float* const meet = reinterpret_cast<float*>(lds) + blk * kRegs * kWave + lane;
+    const auto join = [&](floatx16(&acc)[DH / 32]) {
+      if (part > 0)
 #pragma unroll
-      for (int c = 0; c < kRegs; ++c) {
-        meet[c * kWave] = dk[c / 16][c % 16];
-        meet[(kRegs + c) * kWave] = dv[c / 16][c % 16];
-      }
+        for (int c = 0; c < kRegs; ++c) meet[((part - 1) * BLOCKS * kRegs + c) * kWave] = acc[c / 16][c % 16];
+      __syncthreads();
+      if (part == 0)
+#pragma unroll
+        for (int w = 0; w < PARTS - 1; ++w)
+#pragma unroll
+          for (int c = 0; c < kRegs; ++c) acc[c / 16][c % 16] += meet[(w * BLOCKS * kRegs + c) * kWave];
+    };
+    join(dk);
     __syncthreads();
-    if (part == 1) return;
-#pragma unroll
-    for (int c = 0; c < kRegs; ++c) {
-      dk[c / 16][c % 16] += meet[c * kWave];
-      dv[c / 16][c % 16] += meet[(kRegs + c) * kWave];
-    }
+    join(dv);
+    if (part > 0) return;
   }
   if (!active) return;
-  char* out = lds + blk * (kParts > 1 ? 2 * kRegs * kWave * 4 : kRowsOut<DH>);  // (where it met the others' sums, or a part of the stages)
+  char* out = lds + blk * (PARTS > 1 ? kRegs * kWave * 4 : kRowsOut<DH>);  // (where it met the others' sums, or a part of the stages)
   const int64_t to = my_first * t.tok_stride + t.kvh * t.head_stride;
   store_rows<DH>(out, static_cast<uint16_t*>(t.local ? p.dKl : p.dKn) + to, static_cast<uint32_t>(t.tok_stride * 2), my_rows, dk, p.scale);
   store_rows<DH>(out, static_cast<uint16_t*>(t.local ? p.dVl : p.dVn) + to, static_cast<uint32_t>(t.tok_stride * 2), my_rows, dv, 1.f);
@@ -538,11 +545,12 @@ __global__ __launch_bounds__(kGradThreads, 2) void grad_q_kernel(GradParams p, i
 static_assert(kGradWaves * kRowsOut<128> <= 2 * 2 * TileDims<128>::kBytes && kGradWaves * kRowsOut<64> <= 2 * 2 * TileDims<64>::kBytes,
               "the stages have room for the rows on their way out");
 
-template <int DH, int BLOCKS, bool SHARED>
+template <int DH, int BLOCKS, int PARTS, bool SHARED>
 int launch_kv(const GradParams& p) {
   constexpr int kKeys = 32 * BLOCKS;
-  constexpr int kLds = 2 * (2 * TileDims<DH>::kBytes + kTile * 8) + (SHARED ? 6 * kWave * 4 : 0);
-  static_assert(BLOCKS == 4 || kKeys * DH * 4 * 2 <= kLds, "the stages have room for the sums that meet");
+  constexpr int kLds = 2 * kWalked<PARTS> * (2 * TileDims<DH>::kRowBytes + 8) + (SHARED ? 6 * kWave * 4 : 0);
+  static_assert((PARTS - 1) * kKeys * DH * 4 <= kLds, "the stages have room for the sums that meet");
+  static_assert(kLds * (BLOCKS * PARTS == 8 ? 1 : 2) <= 160 * 1024, "eight wavefronts on a compute unit");
   const int64_t nug_rows = p.shared ? p.Kt : p.max_k, loc_rows = p.shared ? p.Sm : p.max_local;
   const int64_t nug = (nug_rows + kKeys - 1) / kKeys, loc = (loc_rows + kKeys - 1) / kKeys;
   const int64_t owners = (static_cast<int64_t>(p.H_kv) * (p.shared ? 1 : p.B) + 7) / 8 * 8;
@@ -550,15 +558,25 @@ int launch_kv(const GradParams& p) {
   if (nug + loc == 0) return DODO_OK;
   if constexpr (BLOCKS == 4) {
     // 64 keys per workgroup where 128 leave compute units without two of them.  128 / 64 keys, us: 1 sequence of 512 rows, 32 heads, 410
-    // nuggets, 640 local rows 37.5 / 28.5; 64 heads over 8 130 / 85, 4 sequences of it 190 / 130, 8 254 / 251; 1 of 2048, 8 heads, 410, 2048
-    // 71 / 51; 1 of 1000, 32 heads over 8, 1000, 1000 135 / 89, over 32 62 / 74; 8 of 512, 32 heads, 410, 640 152 / 203; 8 of 16, 100, 32
-    // 11 / 20.  (32 keys, by four wavefronts: 84, 71, 267, 509, 82, 138, 176, 564, 61.)
-    if ((nug + loc) * owners < 2 * compute_units()) return launch_kv<DH, 2, SHARED>(p);
+    // nuggets, 640 local rows 37.5 / 28.3; 64 heads over 8 130 / 84, 4 sequences of it 190 / 128, 8 254 / 258; 1 of 2048, 8 heads, 410, 2048
+    // 71 / 50; 1 of 1000, 32 heads over 8, 1000, 1000 135 / 88, over 32 62 / 75; 8 of 512, 32 heads, 410, 640 152 / 203; 8 of 16, 100, 32
+    // 11 / 20.
+    if ((nug + loc) * owners < 2 * compute_units()) {
+      if constexpr (!SHARED) {
+        // Four wavefronts per 32 keys where the longest walk (of at least 16 tiles) would outlast a compute unit's share of all walks.  Two /
+        // four: 1 of 512, 64 heads over 8, 410, 640 84 / 65, 2 of it 90 / 73, 4 128 / 145; 5 of 500, 300, 533 130 / 145, ragged ones up to 777
+        // rows 119 / 99; 1 of 2048, 8 heads, 410, 2048 50 / 43; 1 of 128, 64 over 8, 100, 128 26 / 24, of 64 17 / 21; 1 of 512, 32, 410, 640 28 / 47.
+        const int64_t G = p.H / p.H_kv, longest = G * ((p.max_q + kTile - 1) / kTile), mean = G * ((p.Sq / p.B + kTile - 1) / kTile);
+        const int64_t walks = ((p.Kt + p.Sm) / (2 * 32) + p.B) * p.H_kv;
+        if (longest >= 16 && 5 * longest * compute_units() >= 4 * walks * mean) return launch_kv<DH, 2, 4, SHARED>(p);
+      }
+      return launch_kv<DH, 2, 2, SHARED>(p);
+    }
   }
-  const auto kern = grad_kv_kernel<DH, BLOCKS, SHARED>;
+  const auto kern = grad_kv_kernel<DH, BLOCKS, PARTS, SHARED>;
   const int rc = allow_dynamic_lds(reinterpret_cast<const void*>(kern), kLds);
   if (rc != DODO_OK) return rc;
-  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((nug + loc) * owners)), dim3(kGradThreads), kLds, p.stream, p, static_cast<int>(nug),
+  hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((nug + loc) * owners)), dim3(BLOCKS * PARTS * kWave), kLds, p.stream, p, static_cast<int>(nug),
                      static_cast<int>(loc));
   return launch_status();
 }
@@ -589,7 +607,7 @@ template <int DH>
 int launch_both(const GradParams& p) {
   const int rc = launch_q<DH, 4>(p);  // (first: it makes the rows' statistics)
   if (rc != DODO_OK) return rc;
-  return p.shared ? launch_kv<DH, 4, true>(p) : launch_kv<DH, 4, false>(p);
+  return p.shared ? launch_kv<DH, 4, 1, true>(p) : launch_kv<DH, 4, 1, false>(p);
 }
 
 }  // namespace

@@ -63,6 +63,15 @@ def test_gradients_of_many_sequences(D, H, H_kv, d_h):
     G.check(G.call(D, t, lens, scale), G.reference(t, entries, scale), max(170 * (H // H_kv), 320), d_h, BF16)
 
 
+# (few key rows, and walks of 16 and more tiles of query rows: four wavefronts for 32 keys, two tiles at a time, odd ends)
+@pytest.mark.parametrize("H,H_kv,d_h", [(8, 1, 64), (8, 1, 128), (16, 2, 64), (1, 1, 128)])
+@pytest.mark.parametrize("lens", [([1100], [70], [1100]), ([1025, 3], [0, 65], [1090, 1]), ([1200], [33], [900])])
+def test_gradients_of_long_walks(D, lens, H, H_kv, d_h):
+    scale, entries = d_h ** -0.5, P64.entries_of(*lens)
+    t = G.make(48, *(sum(x) for x in lens), H, H_kv, d_h, BF16, entries, scale)
+    G.check(G.call(D, t, lens, scale), G.reference(t, entries, scale), max(1200 * (H // H_kv), 1200), d_h, BF16)
+
+
 @pytest.mark.parametrize("H,H_kv", [(16, 16), (32, 16)])
 def test_gradients_of_long_texts_in_segments(D, H, H_kv):
     N, seg, tau, every = 4300, 500, 60, 40
