@@ -22,6 +22,21 @@ __device__ __forceinline__ int sequence_of(const int32_t* __restrict__ cu, int B
   return lo;
 }
 
+// The token (of all sequences') that cache row `row` holds, or -1 behind the last sequence's; nugget_idx[row] exists.  Up to 64
+// sequences: everything is fetched at once.  Called by whole wavefronts.
+__device__ __forceinline__ int64_t token_of(const int32_t* __restrict__ cu_seqlens, const int32_t* __restrict__ cu_nuggets,
+                                            const int32_t* __restrict__ nugget_idx, int B, int64_t row) {
+  if (B <= kWave) {
+    const int lane = lane_id();
+    const int bound = cu_nuggets[min(lane + 1, B)], start = cu_seqlens[min(lane, B)], idx = nugget_idx[row];
+    const uint64_t above = __ballot(lane < B && bound > row);
+    if (above == 0) return -1;
+    return static_cast<int64_t>(__builtin_amdgcn_readlane(start, __ffsll(static_cast<long long>(above)) - 1)) + idx;
+  }
+  const int b = sequence_of(cu_nuggets, B, row);
+  return b < 0 ? -1 : static_cast<int64_t>(cu_seqlens[b]) + nugget_idx[row];
+}
+
 // The sequences' token and nugget ranges, found by token.  Up to 64 sequences: a sequence per lane, all of it fetched at once.
 struct SequenceLookup {
   const int32_t *cu_seqlens, *cu_nuggets;

@@ -4,15 +4,16 @@
 // Both are passes over memory.  A thread takes 8 consecutive channels, so the four lanes of a quad hold a block of 32: the block's
 // largest magnitude takes two lane exchanges within the quad, its exponent follows from that number's bits (the mantissa
 // tells whether it is above 1.75, that is 7 / 4), and the conversion instructions divide by the scale and round to nearest,
-// ties to the even index.  8 sequences of 4096 tokens at 10x, 32 heads of 128, bf16: packing 20 us (3.3 TB/s: rows of 8 KiB
-// from memory, behind two lookups; both tensors by one workgroup is no faster), unpacking 10 us (6.9 TB/s).
+// ties to the even index.  8 sequences of 4096 tokens at 10x, 32 heads of 128, bf16: packing 18.7 us (3.6 TB/s: single rows
+// of 8 KiB behind a round of lookups; 20.7 with two rounds and 8 channels a thread; both tensors by one workgroup is no faster), unpacking
+// 10 us (6.9 TB/s).
 #include "dodo_lists.h"
 #include "dodo_q4.h"
 
 namespace dodo {
 namespace {
 
-constexpr int kPackThreads = 512;
+constexpr int kPackThreads = 256;
 
 // Largest of an unsigned number over the four lanes of a quad.
 __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
@@ -56,7 +57,8 @@ __device__ __forceinline__ uint32_t pack8(const float (&x)[8], uint32_t& scale_b
   return bad ? 0u : codes;
 }
 
-// One workgroup per destination row, tensor (the lowest bit of blockIdx.x) and layer (blockIdx.y).
+// One workgroup per destination row, tensor (the lowest bit of blockIdx.x) and layer (blockIdx.y).  A thread requests two units of 8
+// channels before it packs the first.
 template <int DTYPE, bool HEAD_MAJOR>
 __global__ __launch_bounds__(kPackThreads) void gather_q4_kernel(
     const char* __restrict__ K, const char* __restrict__ V, const int32_t* __restrict__ nugget_idx,
@@ -65,24 +67,31 @@ __global__ __launch_bounds__(kPackThreads) void gather_q4_kernel(
     uint8_t* __restrict__ Vc, uint8_t* __restrict__ Vs) {
   const int64_t row = blockIdx.x >> 1, layer = blockIdx.y;
   const bool is_v = blockIdx.x & 1;
-  const int b = sequence_of(cu_nuggets, B, row);
-  if (b < 0) return;  // Kt may be an upper bound of the nugget count
-  const int64_t tok = static_cast<int64_t>(cu_seqlens[b]) + nugget_idx[row];
+  const int64_t tok = token_of(cu_seqlens, cu_nuggets, nugget_idx, B, row);
+  if (tok < 0) return;  // Kt may be an upper bound of the nugget count
   const char* src = (is_v ? V : K) + layer * layer_bytes + tok * token_bytes;
   uint32_t* codes = reinterpret_cast<uint32_t*>(is_v ? Vc : Kc) + layer * Kt * units;
   uint8_t* scales = (is_v ? Vs : Ks) + layer * Kt * (units / 4);
-  for (int u = threadIdx.x; u < units; u += blockDim.x) {  // (units is a multiple of 4: quads stay together)
-    float x[8];
-    load8<DTYPE>(src + static_cast<int64_t>(u) * (DTYPE == DODO_DTYPE_F32 ? 32 : 16), x);
-    uint32_t byte;
-    const uint32_t c = pack8(x, byte);
-    int64_t at = row * units + u;
-    if (HEAD_MAJOR) {
-      const int h = u / units_per_head;
-      at = (static_cast<int64_t>(h) * Kt + row) * units_per_head + (u - h * units_per_head);
+  constexpr int kUnitBytes = DTYPE == DODO_DTYPE_F32 ? 32 : 16;
+  for (int u0 = threadIdx.x; u0 < units; u0 += 2 * blockDim.x) {  // (units is a multiple of 4: quads stay together)
+    const int u1 = u0 + static_cast<int>(blockDim.x);
+    float x[2][8];
+    load8<DTYPE>(src + static_cast<int64_t>(u0) * kUnitBytes, x[0]);
+    if (u1 < units) load8<DTYPE>(src + static_cast<int64_t>(u1) * kUnitBytes, x[1]);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int u = c == 0 ? u0 : u1;
+      if (u >= units) break;
+      uint32_t byte;
+      const uint32_t w = pack8(x[c], byte);
+      int64_t at = row * units + u;
+      if (HEAD_MAJOR) {
+        const int h = u / units_per_head;
+        at = (static_cast<int64_t>(h) * Kt + row) * units_per_head + (u - h * units_per_head);
+      }
+      codes[at] = w;
+      if ((u & 3) == 0) scales[at >> 2] = static_cast<uint8_t>(byte);
     }
-    codes[at] = c;
-    if ((u & 3) == 0) scales[at >> 2] = static_cast<uint8_t>(byte);
   }
 }
 
@@ -123,7 +132,7 @@ int gather_q4_entry(const void* K, const void* V, int dtype, const int32_t* nugg
   if (!aligned16(K) || !aligned16(V) || !aligned16(Kc) || !aligned16(Vc)) return DODO_ERR_UNSUPPORTED;
   if (((reinterpret_cast<uintptr_t>(Ks) | reinterpret_cast<uintptr_t>(Vs)) & 3u) != 0) return DODO_ERR_UNSUPPORTED;
   const int units_per_head = d_h / 8, units = units_per_head * H_kv;
-  // as many threads as units, up to eight wavefronts
+  // as many threads as units, up to four wavefronts
   const int threads = units >= kPackThreads ? kPackThreads : (units + kWave - 1) / kWave * kWave;
   const dim3 grid(static_cast<unsigned>(2 * Kt), static_cast<unsigned>(L)), block(static_cast<unsigned>(threads));
   const auto launch = [&](auto kern) {
