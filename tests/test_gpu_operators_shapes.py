@@ -159,3 +159,16 @@ def test_a_training_step_from_the_context_on(D, dtype):
         rest = torch.ones(N, dtype=torch.bool, device=dev())
         rest[tok] = False
         assert torch.equal(x[tok], g) and not bool(x[rest].any())
+
+
+def test_packing_of_more_sequences_than_lanes(D):
+    n_lens = [1 + (13 * b) % 40 for b in range(90)]
+    k_lens = [min(n, b % 4) for b, n in enumerate(n_lens)]
+    K, V = W.normal(61, 0, (sum(n_lens), 2, 64), 1.0, BF16, dev()), W.normal(61, 1, (sum(n_lens), 2, 64), 1.0, BF16, dev())
+    lists = [sorted((7 * i + b) % n for i in range(k)) for b, (n, k) in enumerate(zip(n_lens, k_lens))]
+    idx = torch.tensor([i for l in lists for i in l], dtype=torch.int32, device=dev())
+    got = D.dodo_gather_nuggets_q4(K, V, idx, W.cumulative(n_lens, dev()), W.cumulative(k_lens, dev()), sum(k_lens))
+    starts = W.cumulative(n_lens, dev()).tolist()
+    tokens = [starts[b] + i for b, l in enumerate(lists) for i in l]
+    want = [x for t in (K, V) for x in P64.quantise_q4(t.cpu()[tokens])]
+    assert all(torch.equal(x.cpu(), y) for x, y in zip(got, want))
