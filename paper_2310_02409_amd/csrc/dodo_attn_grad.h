@@ -105,17 +105,7 @@ __device__ __forceinline__ SeenBy seen_by(const GradParams& p, const KeyTile& t,
 // bf16, on the bf16 matrix instructions.
 int launch_grad_mfma(const GradParams& p, int32_t d_h);
 
-// Four consecutive elements from i on as fp32, and the reverse (16 or 8 bytes, aligned to as much).
-template <int DTYPE>
-__device__ __forceinline__ void load4(const void* p, int64_t i, float (&x)[4]) {
-  if (DTYPE == DODO_DTYPE_F32) {
-    const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-  } else {
-    const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
-    x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
-  }
-}
+// Four fp32 numbers to elements i to i + 3 (16 or 8 bytes, aligned to as much).
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 template <int DTYPE>

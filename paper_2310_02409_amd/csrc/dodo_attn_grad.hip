@@ -40,10 +40,8 @@ template <int DH>
 __device__ __forceinline__ void load_row(const void* base, int64_t off, float (&f)[DH / 4]) {
 #pragma unroll
   for (int s = 0; s < DH / 16; ++s) {
-    float x[4];
-    load4<DODO_DTYPE_F32>(base, off + 16 * s, x);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[4 * s + e] = x[e];
+    const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + off + 16 * s);
+    f[4 * s] = x.x; f[4 * s + 1] = x.y; f[4 * s + 2] = x.z; f[4 * s + 3] = x.w;
   }
 }
 __device__ __forceinline__ floatx4 mfma(float a, float b, const floatx4& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
@@ -62,10 +60,11 @@ template <int DH>
 __device__ __forceinline__ void add_column(OutBlocks<DH>& acc, const void* base, int64_t off, float w) {
 #pragma unroll
   for (int hi = 0; hi < DH / 64; ++hi) {
-    float x[4];
-    load4<DODO_DTYPE_F32>(base, off + 64 * hi, x);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[4 * hi + e] = mfma(x[e], w, acc[4 * hi + e]);
+    const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + off + 64 * hi);
+    acc[4 * hi] = mfma(x.x, w, acc[4 * hi]);
+    acc[4 * hi + 1] = mfma(x.y, w, acc[4 * hi + 1]);
+    acc[4 * hi + 2] = mfma(x.z, w, acc[4 * hi + 2]);
+    acc[4 * hi + 3] = mfma(x.w, w, acc[4 * hi + 3]);
   }
 }
 

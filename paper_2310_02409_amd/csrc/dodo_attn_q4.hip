@@ -6,7 +6,7 @@
 //   K      codes go straight to registers: the sum over channels may run in any order, so a lane takes consecutive channels of
 //          its key, whose codes are one load and whose scale is one byte (two bytes for 64 channels), and the query vectors'
 //          fragments follow that order.  A conversion turns two codes into two bf16 numbers, scale included, exactly.
-//   S^T = K Q^T, online softmax in base 2, O^T += V^T P^T with the weights in two bf16 parts: as in dodo_attn_group.hip
+//   S^T = K Q^T, online softmax in base 2, O^T += V^T P^T with the weights in two bf16 parts: as in dodo_attn_group.h and .hip
 //   V      has to be turned around: its codes are converted as they come (32 channels, one scale a lane), written to LDS and read back
 //          through the transposing read.
 // Local rows, which are bf16, go through the same LDS by direct loads, K and V in turn, each requested as soon as its half of
