@@ -23,4 +23,21 @@ __device__ __forceinline__ uint4 unpack8_bf16(uint32_t codes, float scale) {
   return v;
 }
 
+// The scale bytes of a row and head (BLOCKS of them, aligned to as many), the first one lowest; and whether one is kScaleBadQ4.
+template <int BLOCKS>
+__device__ __forceinline__ uint32_t row_scales_q4(const uint8_t* scales, int64_t row_head) {
+  static_assert(BLOCKS == 2 || BLOCKS == 4, "64 or 128 channels");
+  if (BLOCKS == 2) return reinterpret_cast<const uint16_t*>(scales)[row_head];
+  return reinterpret_cast<const uint32_t*>(scales)[row_head];
+}
+__device__ __forceinline__ bool any_bad_q4(uint32_t scales) {
+  static_assert(kScaleBadQ4 == 255, "all bits of a byte");
+  return ((~scales - 0x01010101u) & scales & 0x80808080u) != 0;  // a byte of ~scales is 0
+}
+
+// dodo_unpack_nuggets_q4; `for_attention` (d_h 64 or 128): a K/V row and head with a bad block in K is all zeros there in that block, and
+// NaN in all channels of V.
+int unpack_q4(const uint8_t* Kc, const uint8_t* Ks, const uint8_t* Vc, const uint8_t* Vs, int64_t rows, int32_t d_h, int dtype,
+              bool for_attention, void* Kn, void* Vn, void* stream);
+
 }  // namespace dodo

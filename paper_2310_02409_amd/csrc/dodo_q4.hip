@@ -7,6 +7,8 @@
 // ties to the even index.  8 sequences of 4096 tokens at 10x, 32 heads of 128, bf16: packing 18.7 us (3.6 TB/s: single rows
 // of 8 KiB behind a round of lookups; 20.7 with two rounds and 8 channels a thread; both tensors by one workgroup is no faster), unpacking
 // 10 us (6.9 TB/s).
+#include <type_traits>
+
 #include "dodo_lists.h"
 #include "dodo_q4.h"
 
@@ -95,15 +97,26 @@ __global__ __launch_bounds__(kPackThreads) void gather_q4_kernel(
   }
 }
 
-// A thread reads the codes of 8 channels of K (blockIdx.y = 0) or V.
-template <int DTYPE>
+// A thread reads the codes of 8 channels of K (blockIdx.y = 0) or V.  BLOCKS = 0: what they stand for.  BLOCKS (2 or 4) scale bytes a row
+// and head: for the attention kernels, which answer a NaN among their logits each in its own way, but all hand on one in V.  So a
+// bad block of K becomes zeros, and that row and head of V NaN in all channels.  Without / with: 8 sequences of 410 nuggets, 32 heads of 128, bf16
+// 8.9 / 8.9 us; 32 of 3277, 8 heads of 128, fp32 345 / 392.
+template <int DTYPE, int BLOCKS>
 __global__ __launch_bounds__(256) void unpack_q4_kernel(const uint32_t* __restrict__ Kc, const uint8_t* __restrict__ Ks,
                                                         const uint32_t* __restrict__ Vc, const uint8_t* __restrict__ Vs,
                                                         int64_t units, void* __restrict__ Kn, void* __restrict__ Vn) {
   const int64_t u = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (u >= units) return;
-  const uint32_t codes = (blockIdx.y ? Vc : Kc)[u];
-  const uint32_t byte = (blockIdx.y ? Vs : Ks)[u >> 2];
+  uint32_t codes = (blockIdx.y ? Vc : Kc)[u];
+  uint32_t byte = (blockIdx.y ? Vs : Ks)[u >> 2];
+  if constexpr (BLOCKS > 0) {
+    if (blockIdx.y) {
+      if (any_bad_q4(row_scales_q4<BLOCKS>(Ks, u / (4 * BLOCKS)))) byte = kScaleBadQ4;
+    } else if (byte == kScaleBadQ4) {
+      codes = 0;
+      byte = 127;
+    }
+  }
   const uint4 v = unpack8_bf16(codes, scale_q4(byte));
   void* out = blockIdx.y ? Vn : Kn;
   if (DTYPE == DODO_DTYPE_BF16) {
@@ -169,22 +182,36 @@ extern "C" int dodo_gather_nuggets_q4_layers(const void* K, const void* V, int d
                                src_layer_stride, Kc, Ks, Vc, Vs, layout, stream);
 }
 
-extern "C" int dodo_unpack_nuggets_q4(const uint8_t* Kc, const uint8_t* Ks, const uint8_t* Vc, const uint8_t* Vs, int64_t rows,
-                                      int32_t d_h, int dtype, void* Kn, void* Vn, void* stream) {
-  using namespace dodo;
+namespace dodo {
+
+int unpack_q4(const uint8_t* Kc, const uint8_t* Ks, const uint8_t* Vc, const uint8_t* Vs, int64_t rows, int32_t d_h, int dtype,
+              bool for_attention, void* Kn, void* Vn, void* stream) {
   if (rows < 0 || d_h <= 0) return DODO_ERR_INVALID_ARG;
   if (rows == 0) return DODO_OK;
   if (!Kc || !Ks || !Vc || !Vs || !Kn || !Vn) return DODO_ERR_INVALID_ARG;
   if (!dtype_ok(dtype) || d_h % kBlockQ4 != 0) return DODO_ERR_UNSUPPORTED;
   if (!aligned16(Kc) || !aligned16(Vc) || !aligned16(Kn) || !aligned16(Vn)) return DODO_ERR_UNSUPPORTED;
   if (rows > 0x7fffffffLL * 32 / (d_h / 8)) return DODO_ERR_UNSUPPORTED;
+  if (for_attention && d_h != 64 && d_h != 128) return DODO_ERR_UNSUPPORTED;
   const int64_t units = rows * (d_h / 8);
   const dim3 grid(static_cast<unsigned>((units + 255) / 256), 2), block(256);
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  const uint32_t *kc = reinterpret_cast<const uint32_t*>(Kc), *vc = reinterpret_cast<const uint32_t*>(Vc);
-  if (dtype == DODO_DTYPE_F32)
-    hipLaunchKernelGGL(unpack_q4_kernel<DODO_DTYPE_F32>, grid, block, 0, s, kc, Ks, vc, Vs, units, Kn, Vn);
-  else
-    hipLaunchKernelGGL(unpack_q4_kernel<DODO_DTYPE_BF16>, grid, block, 0, s, kc, Ks, vc, Vs, units, Kn, Vn);
+  const auto launch = [&](auto kern) {
+    hipLaunchKernelGGL(kern, grid, block, 0, static_cast<hipStream_t>(stream), reinterpret_cast<const uint32_t*>(Kc), Ks,
+                       reinterpret_cast<const uint32_t*>(Vc), Vs, units, Kn, Vn);
+  };
+  const auto launch_as = [&](auto blocks) {
+    constexpr int kBlocks = decltype(blocks)::value;
+    if (dtype == DODO_DTYPE_F32) launch(unpack_q4_kernel<DODO_DTYPE_F32, kBlocks>); else launch(unpack_q4_kernel<DODO_DTYPE_BF16, kBlocks>);
+  };
+  if (!for_attention) launch_as(std::integral_constant<int, 0>{});
+  else if (d_h == 64) launch_as(std::integral_constant<int, 2>{});
+  else launch_as(std::integral_constant<int, 4>{});
   return launch_status();
+}
+
+}  // namespace dodo
+
+extern "C" int dodo_unpack_nuggets_q4(const uint8_t* Kc, const uint8_t* Ks, const uint8_t* Vc, const uint8_t* Vs, int64_t rows,
+                                      int32_t d_h, int dtype, void* Kn, void* Vn, void* stream) {
+  return dodo::unpack_q4(Kc, Ks, Vc, Vs, rows, d_h, dtype, false, Kn, Vn, stream);
 }
