@@ -443,7 +443,8 @@ int dodo_gather_nuggets_grad_layers(const void* dKn, const void* dVn, int dtype,
  * all of its channels read as NaN (its codes are 0).  Channel 2i sits in the lower four bits of byte i.  A row and head take
  * d_h / 2 + d_h / 32 bytes (4.25 bits a channel, 3.76 times less than bf16), codes and scales in two arrays:
  *   Kc, Vc  [Kt, H_kv, d_h / 2] (token-major) or [H_kv, Kt, d_h / 2] (head-major) bytes, 16-byte aligned
- *   Ks, Vs  [Kt, H_kv, d_h / 32] or [H_kv, Kt, d_h / 32] bytes, 4-byte aligned
+ *   Ks, Vs  [Kt, H_kv, d_h / 32] or [H_kv, Kt, d_h / 32] bytes, 4-byte aligned for packing; attention wants the scales of a row and
+ *           head aligned (d_h / 32 bytes), so that it also reads every layer of dodo_gather_nuggets_q4_layers where it lies
  * Every value is a bf16 number (and an fp32 one), so that reading a cache back rounds nothing.
  *
  * dodo_gather_nuggets_q4 is dodo_gather_nuggets into such a cache (d_h a multiple of 32).

@@ -605,7 +605,7 @@ extern "C" int dodo_nugget_attention_q4(const void* Q, const uint8_t* Kc, const 
   if (!dtype_ok(dtype)) return DODO_ERR_UNSUPPORTED;
   if (d_h != 64 && d_h != 128) return DODO_ERR_UNSUPPORTED;
   if (!aligned16(Q) || !aligned16(O) || !aligned16(Kc) || !aligned16(Vc) || !aligned16(Kl) || !aligned16(Vl) || !aligned16(ws) ||
-      ((reinterpret_cast<uintptr_t>(Ks) | reinterpret_cast<uintptr_t>(Vs)) & 3u) != 0)
+      ((reinterpret_cast<uintptr_t>(Ks) | reinterpret_cast<uintptr_t>(Vs)) & (d_h / kBlockQ4 - 1)) != 0)  // (2 or 4 scales a row and head)
     return DODO_ERR_UNSUPPORTED;
   const size_t need = dodo_nugget_attention_q4_workspace_bytes(B, H, H_kv, d_h, max_q, max_k, max_local, Kt, dtype);
   if (need > 0 && (!ws || ws_bytes < need)) return DODO_ERR_WORKSPACE_TOO_SMALL;
