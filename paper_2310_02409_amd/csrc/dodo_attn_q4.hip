@@ -481,20 +481,23 @@ __global__ void clear_words_kernel(uint32_t* __restrict__ p, int64_t n) {
 }
 
 // Unpacked caches: the attention kernels know nothing of bad blocks, which the unpacking has put into V, so that their log-sum-exp is made
-// NaN afterwards, where the caller asks for it.  A workgroup per sequence and K/V head looks through its scales of K: 2.4 us for a sequence of 410
-// nuggets, 32 heads of 128, 6 for 8 of them or for 32 of 3277, 8 heads.
+// NaN afterwards, where the caller asks for it.  A workgroup looks through up to kMarked scales of K of a sequence and K/V head; all that
+// find one write the same.  3 us for a sequence of 410 nuggets, 32 heads of 128, 5 for 8 of them or for 32 of 3277, 8 heads.
+constexpr int kMarkThreads = 256, kMarked = 4 * kMarkThreads;
 template <int BLOCKS>
-__global__ __launch_bounds__(256) void mark_lse_kernel(const uint8_t* __restrict__ Ks, const int32_t* __restrict__ cu_q,
-                                                       const int32_t* __restrict__ cu_nuggets, int64_t n_pairs, int H_kv, int G,
-                                                       int64_t row_stride, int64_t head_stride, float* __restrict__ lse) {
-  for (int64_t pair = blockIdx.x; pair < n_pairs; pair += gridDim.x) {
-    const int64_t b = pair / H_kv, kvh = pair % H_kv, k0 = cu_nuggets[b], k_end = cu_nuggets[b + 1];
+__global__ __launch_bounds__(kMarkThreads) void mark_lse_kernel(const uint8_t* __restrict__ Ks, const int32_t* __restrict__ cu_q,
+                                                                const int32_t* __restrict__ cu_nuggets, int64_t n_items, int n_parts, int H_kv, int G,
+                                                                int64_t row_stride, int64_t head_stride, float* __restrict__ lse) {
+  for (int64_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+    const int64_t part = item % n_parts, pair = item / n_parts, b = pair / H_kv, kvh = pair % H_kv;
+    const int64_t q0 = cu_q[b], q_end = cu_q[b + 1], k0 = cu_nuggets[b], k_end = cu_nuggets[b + 1];
+    if (q_end <= q0) continue;
     int bad = 0;
-    for (int64_t i = k0 + threadIdx.x; i < k_end; i += 256)
+#pragma unroll 4
+    for (int64_t i = k0 + part * kMarkThreads + threadIdx.x; i < k_end; i += static_cast<int64_t>(n_parts) * kMarkThreads)
       bad |= any_bad_q4(row_scales_q4<BLOCKS>(Ks, i * row_stride + kvh * head_stride)) ? 1 : 0;
     if (!__syncthreads_or(bad)) continue;
-    const int64_t q0 = cu_q[b], count = (cu_q[b + 1] - q0) * G;
-    for (int64_t i = threadIdx.x; i < count; i += 256) lse[((q0 + i / G) * H_kv + kvh) * G + i % G] = __builtin_nanf("");
+    for (int64_t i = threadIdx.x; i < (q_end - q0) * G; i += kMarkThreads) lse[((q0 + i / G) * H_kv + kvh) * G + i % G] = __builtin_nanf("");
   }
 }
 
@@ -650,10 +653,10 @@ extern "C" int dodo_nugget_attention_q4(const void* Q, const uint8_t* Kc, const 
   const int rc = dodo_nugget_attention(Q, Kn, Vn, Kl, Vl, cu_q, cu_nuggets, cu_local, B, H, H_kv, d_h, max_q, max_k, max_local, Kt,
                                        softmax_scale, dtype, layout, O, lse, attention ? att_ws : nullptr, attention, stream);
   if (rc != DODO_OK || lse == nullptr || Kt == 0 || max_k == 0) return rc;
-  const int64_t pairs = static_cast<int64_t>(B) * H_kv;
+  const int64_t parts = (static_cast<int64_t>(max_k) + kMarked - 1) / kMarked, items = parts * B * H_kv;
   const auto mark = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(std::min<int64_t>(pairs, 1 << 20))), dim3(256), 0, s, Ks, cu_q, cu_nuggets, pairs, H_kv, H / H_kv,
-                       layout == DODO_LAYOUT_TOKEN_MAJOR ? static_cast<int64_t>(H_kv) : int64_t{1},
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(std::min<int64_t>(items, 1 << 20))), dim3(kMarkThreads), 0, s, Ks, cu_q, cu_nuggets, items,
+                       static_cast<int>(parts), H_kv, H / H_kv, layout == DODO_LAYOUT_TOKEN_MAJOR ? static_cast<int64_t>(H_kv) : int64_t{1},
                        layout == DODO_LAYOUT_TOKEN_MAJOR ? int64_t{1} : Kt, lse);
   };
   if (d_h == 128) mark(mark_lse_kernel<4>); else mark(mark_lse_kernel<2>);
