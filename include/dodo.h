@@ -475,8 +475,9 @@ int dodo_unpack_nuggets_q4(const uint8_t* Kc, const uint8_t* Ks, const uint8_t* 
  * Few query rows (bf16, H / H_kv <= 32, and max_q < DODO_ATTENTION_BLOCK_MIN_Q or max_q * H / H_kv <= 128) read the codes where
  * they are; other calls unpack the cache into the workspace first.  Deterministic.  Supported: d_h in {64, 128}, fp32 or bf16.
  * A block whose scale byte is 255 makes NaN of the heads' rows that see it, lse with them (K), or of its 32 channels of these
- * rows and of no lse (V).  Kl and Vl should be finite: a NaN or an infinity there reaches the rows of its sequence and K/V head
- * that see it, and may reach those before it.
+ * rows and of no lse (V), on every route.  Q, Kl and Vl should be finite: where the codes are read in place, a NaN or an infinity in
+ * Kl or Vl reaches the rows of its sequence and K/V head that see it, and may reach those before it; other calls are with it
+ * as dodo_nugget_attention, which may pass over it.
  * ws: dodo_nugget_attention_q4_workspace_bytes bytes (may be 0), 16-byte aligned, the first DODO_Q4_ZEROED_BYTES of it (or all, where
  * it is smaller) filled with zeros before its first use.  A call leaves these as zeros, so any later call that the size serves can
  * use it as it is; after a call that was aborted they are filled again.  It must not be shared by calls that may overlap in time.

@@ -72,3 +72,26 @@ def test_reading_back_a_bad_key_leaves_its_value(D):
         want = torch.zeros(9, 2, 64, dtype=torch.bool, device="cuda")
         want[4, 1, :32] = True
         assert torch.equal(torch.isnan(Kn), want) and not bool(torch.isnan(Vn).any())
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("H,H_kv,q,m", [(4, 2, 1, 40), (8, 2, 9, 50), (2, 2, 60, 100)])
+def test_a_local_row_that_is_not_finite(D, H, H_kv, q, m, value):
+    """Codes read in place: it reaches the rows of its sequence and K/V head that see it, and no other sequence's or head's."""
+    lens, d_h, at = ([q, q, q], [70, 300, 40], [m, m, m]), 64, m - 1 - q // 2  # (a row that the later half of the query rows sees)
+    t = Q4.attention_case(73, *lens, H, H_kv, d_h, BF16)
+    t["Q"][..., 3] = t["Q"][..., 3].abs() + 0.5  # (an infinite channel of K makes an infinite logit, of one sign)
+    good, good_lse = Q4.attend(D, t, lens, 0.125, want_lse=True)
+    G, first = H // H_kv, 2 * q - 1 - q // 2  # of the second sequence's query rows, the first one that sees it
+    for name in ("Kl", "Vl"):
+        bad = {n: v.clone() for n, v in t.items()}
+        bad[name][m + at, 1, 3] = value
+        O, lse = Q4.attend(D, bad, lens, 0.125, want_lse=True)
+        rows, other = torch.zeros_like(lse, dtype=torch.bool), torch.ones_like(lse, dtype=torch.bool)
+        rows[first:2 * q, G:2 * G] = True
+        other[q:2 * q, G:2 * G] = False
+        assert torch.equal(O[other], good[other]) and torch.equal(lse[other], good_lse[other]), name
+        if name == "Kl":
+            assert torch.isnan(O[rows].float()).all() and not torch.isfinite(lse[rows]).any()
+        else:
+            assert not torch.isfinite(O[rows].float())[:, 3].any() and torch.equal(lse[rows], good_lse[rows])
