@@ -22,8 +22,9 @@ namespace {
 // rows, 16 a wavefront, walked together, is slower where it leaves compute units idle and little faster elsewhere.  This / that, dQ
 // and dK with dV, us: 1 sequence, 4 heads of 64, 32 rows, 51 nuggets, 48 local rows 6.7 + 6.7 / 10.5 + 9.2; 8 sequences, 32 heads of 128,
 // 512 rows, 410 nuggets, 640 local rows 1256 + 1422 / 1169 + 1379; 2, 2048 rows, 410, 2048 1871 + 2291 / 2490 + 2508; 8, 128 rows, 100, 256
-// 140 + 187 / 110 + 168.)  The large ones run at half of the fp32 matrix rate, 70 TFLOP/s; the smallest are a chain of loads: the
-// ranges, the owned rows, the walked rows, some 2 us each with the launch.
+// 140 + 187 / 110 + 168.)  The large ones run at half of the fp32 matrix rate, 70 TFLOP/s: the fragments come through the vector memory path,
+// whose data return is busy in 86% (dQ) and 95% (dK, dV) of the cycles, the matrix pipes in 43 and 51.  The smallest are a chain of
+// loads: the ranges, the owned rows, the walked rows, some 2 us each with the launch.
 
 constexpr int kPlainRows = 16;  // owned by a workgroup
 template <int DH>

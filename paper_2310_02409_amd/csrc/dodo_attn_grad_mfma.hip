@@ -8,11 +8,19 @@
 // bytes a lane) for S and dP, and columns (transposing reads of 8 bytes) for the second products.  Its 16-byte pieces are
 // swizzled so that both are free of bank conflicts.  The owned rows' fragments and the sums stay in registers.
 //
+// P and dS are rounded to bf16 once before the second products: half a step, 2^-8, of each term, which leaves the gradients
+// an error of 2.4e-3 against 64 bits (2-norm; the rounding of the results alone gives 1.7e-3).  With what they lack as a second bf16 part
+// the error is 1.7e-3, and the second products are done twice, with 20 to 40 registers more than there are in the kernel for dK and dV.
+// Once / twice: 8 sequences of 512 rows, 32 heads, 410 nuggets, 640 local rows 245 / 356 us; 16 of 2048, 40, 103, 2048 2.80 / 4.21 ms; 5 of up to
+// 777, 64 over 8 160 / 297 us; segments of 4 texts, 32 690 / 1045 us.
+//
 // What bounds them: a wavefront with 32 owned rows of 128 channels fills its registers, so every matrix instruction comes with 16 bytes a
-// lane from LDS, and LDS is as busy as the matrix pipes; in long calls the card lowers its clock to 1.9 GHz besides.  16 sequences of
-// 2048 rows, 40 heads of 128 (5 products: 1.89 TFLOP): 2.76 ms, 680 TFLOP/s of the 5 products and 950 of the 7 executed, where a large
-// library product reaches 1180 to 1360.  (64 owned rows a wavefront, tiles of 128 rows, or the second products one tile later: slower, by
-// spills or by fewer wavefronts.)
+// lane from LDS, and a SIMD has two wavefronts to cover the chain LDS, products, exp2, products of each other; in long calls the card lowers its
+// clock to 1.75 to 1.9 GHz besides.  16 sequences of 2048 rows, 40 heads of 128 (5 products: 1.89 TFLOP): 2.80 ms, 675 TFLOP/s of the 5 products
+// and 945 of the 7 executed, where a large library product reaches 1180 to 1360.  Counters there (dQ; dK, dV): matrix pipes busy in 44 and 54% of
+// the cycles, LDS reading in 23 and 36, wavefronts waiting in 23 and 33% of theirs.  8 sequences of 512 rows: pipes 32 and 34%, and
+// compute units without any work in 22 and 20%, the start and the end of the launch.  (64 owned rows a wavefront, tiles of 128 rows, or the
+// second products one tile later: slower, by spills or by fewer wavefronts.)
 #include <type_traits>
 
 #include "dodo_attn_grad.h"

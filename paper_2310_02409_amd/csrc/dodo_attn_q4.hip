@@ -15,7 +15,7 @@
 // order of their shares: nothing waits, and the order of the sums does not depend on who is last.
 //
 // What bounds it: memory where the cache is large (a decode step of 32 ragged sequences, 64 heads over 8, up to 3277 nuggets: 34.4
-// us over fresh caches, 3.5 TB/s; 32 equal ones 40 us, 3.7 TB/s, by heads 33 us, 4.4 TB/s, since token by token a head's codes are half
+// to 35.8 us over fresh caches, 3.4 TB/s; 32 equal ones 40 us, 3.7 TB/s, by heads 33 us, 4.4 TB/s, since token by token a head's codes are half
 // a cache line); a chain of latencies where it is small (1 sequence, 32 heads, 410 nuggets 8.3 us: ranges, queries and codes, a tile or
 // two, the shares' meeting).
 //
@@ -80,7 +80,7 @@ template <int N>
 struct Codes {
   uint32_t w[N];
 };
-// N words of codes (4, 8 or 16 bytes each aligned to as much, up to 32 bytes)
+// N words of codes: 8 bytes, or 16 or 32 in pieces of 16, aligned to the piece
 template <int N>
 __device__ __forceinline__ Codes<N> load_codes(const uint8_t* p) {
   Codes<N> c;
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void attention_q4_kernel(Q4Args a) {
   };
   const int t0 = a.nsplit == 1 ? 0 : tile_at(split), t1 = a.nsplit == 1 ? n_tiles : tile_at(split + 1);
   const int nug_end = min(t1, n_nug);
-  // tiles t0 + wave, t0 + wave + 4, ...: first nuggets, then (from local tile l_first on) local rows
+  // tiles t0 + wave, t0 + wave + NW, ...: first nuggets, then (from local tile l_first on) local rows
   const int first = t0 + wave;
   const int skip = first < n_nug ? (n_nug - first + NW - 1) / NW * NW : 0;
   const int l_first = first + skip - n_nug, l_end_tile = t1 - n_nug;

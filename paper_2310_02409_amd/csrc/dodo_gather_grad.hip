@@ -2,12 +2,13 @@
 // row p of the cache, so the gradient of a token's row is the sum of the cache rows whose index it is: one row for a nugget, none
 // for the other tokens (nine in ten at the usual compression), more where a list holds an index twice.
 //
-// A pass over memory that mostly writes zeros.  Without accumulation a workgroup writes the rows of kTokens consecutive tokens of
-// K or of V: one search in the sequence's ascending list for the first of them, then the list is read on from
+// A pass over memory that mostly writes zeros.  Without accumulation a workgroup writes the rows of kTokens consecutive tokens, of
+// K and of V: one search in the sequence's ascending list for the first of them, then the list is read on from
 // there, one entry per lane, and a ballot tells each token how many rows are its own.  So no row is written twice and
 // there are no atomics, and a list with repeated indices gives the same sum every time.  8 sequences of 4096 tokens at 10x, 32 heads of
 // 128, bf16: 114 us, 5.2 TB/s of the bytes that have to move (a fill reaches 6.9, a copy 4.9); a workgroup per token and tensor took 155.  With accumulation only
-// the nuggets' tokens are touched: one workgroup per cache row, of which the first of a run of equal indices adds the run.
+// the nuggets' tokens are touched: one workgroup per cache row and tensor, of which the first of a run of equal indices adds the run; 4 sequences
+// of 3500 to 4096 tokens at 10x, 32 heads of 128, bf16: 22 us, 3.3 TB/s (each row waits for a round of lookups and then for two reads).
 #include "dodo_lists.h"
 
 namespace dodo {
@@ -79,7 +80,7 @@ struct GradRows {
   int64_t Kt, token_vec, src_layer_vec, dst_layer_vec;
 };
 
-// Grid: (chunk of kTokens tokens; layer), K and V.
+// Grid: (chunk of kTokens tokens; layer).
 template <int DTYPE, bool HEAD_MAJOR>
 __global__ __launch_bounds__(kMaxThreads) void scatter_rows_kernel(GradRows a) {
   const uint4 *dKn = a.dKn + blockIdx.y * a.src_layer_vec, *dVn = a.dVn + blockIdx.y * a.src_layer_vec;

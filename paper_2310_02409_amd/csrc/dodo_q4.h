@@ -9,7 +9,7 @@ constexpr uint32_t kScaleBadQ4 = 255;  // scale byte of a block with a NaN or an
 constexpr int kLeastExpQ4 = -125;     // exponents of a scale: no value but 0 is below 2^-126, the least normal number,
 constexpr int kMostExpQ4 = 125;       // and none overflows (6 * 2^125; with 126 a 3.9 would round to 4 * 2^126)
 
-// The scale 2^(byte - 127) as fp32 (bytes 2 .. 254; for 255 an infinity, with which the conversions below give NaN for every code).
+// The scale 2^(byte - 127) as fp32 (bytes 2 .. 252; for 255 an infinity, with which the conversions below give NaN for every code).
 __device__ __forceinline__ float scale_q4(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // Eight channels (the codes of 4 bytes, the lowest first) as four pairs of bf16.  The conversion multiplies by the scale's power of
